@@ -187,6 +187,53 @@ mote_status_t mote_route_stats(const float* logits, const int32_t* topk_idx, int
                                int32_t* tokens_per_expert, float* prob_sum, void* stream);
 
 /* ------------------------------------------------------------------------------------------------
+ * mote_route_scored -- router with softmax or sigmoid scores, a bias for balance, groups of experts and
+ * renormalised weights (the forms that later MoE models give Eq. 3):
+ *
+ *   l = Wr x + logit_bias                                fp32 accumulation of exact products
+ *   s = softmax(l) over all E experts, or 1 / (1 + exp(-l))
+ *   c = s + select_bias                                  takes part in the choice, not in the weights
+ *   groups   : the experts in n_groups runs of E / n_groups; a group counts the sum of its two largest c (its one c
+ *              if it has one expert); the topk_groups largest stay, ties to the lower group
+ *   choice   : the k largest c among the experts of those groups, in descending order, ties to the lower expert
+ *              index.  Without select_bias and groups the order is that of the logits.
+ *   w_j      = scale * s_j / max(sum of the k chosen s, 1e-20) if renorm, else scale * s_j
+ *
+ * The choice is that of exact arithmetic: where fp32 scores are too close to tell, the logits concerned are evaluated
+ * again in 64 bits, so the same token gets the same experts in every batch and on every path.
+ * logit_bias and select_bias may hold -inf: such an expert is chosen only where fewer than k others are left.
+ *
+ *   Wr      [E, d], w_dtype MOTE_DTYPE_F32 or MOTE_DTYPE_BF16, 16-B aligned; logit_bias, select_bias [E] float or NULL
+ *   packed  output of mote_router_pack for this Wr, 256-B aligned
+ *   x_bf16  in   [T, d] bf16, row stride ldx elements (ldx >= d, ldx % 8 == 0), 16-B aligned
+ *   topk_idx out [T, k] int32;  topk_w out [T, k] float;  logits out [T, E] float or NULL
+ * T = 0 is a no-op.  Errors: d % 8 != 0, d > 32768, E < 1, E > MOTE_MAX_EXPERTS, k < 1, k > E, k > MOTE_MAX_TOPK, n_groups not
+ * a divisor of E, topk_groups not in 1 .. n_groups, k > topk_groups * E / n_groups, unknown scoring, a scale that is not a
+ * number -> ERR_SHAPE; ERR_DTYPE; ERR_NULL; ERR_ALIGN.
+ */
+enum { MOTE_SCORE_SOFTMAX = 0, MOTE_SCORE_SIGMOID = 1 };
+typedef struct {
+  int32_t d, E, k;
+  int32_t scoring;                 /* MOTE_SCORE_*                                              */
+  int32_t n_groups, topk_groups;   /* 1, 1: no groups                                           */
+  int32_t renorm;
+  float scale;
+  const void* Wr;                  /* [E, d]                                                    */
+  int32_t w_dtype;                 /* MOTE_DTYPE_*                                              */
+  const float* logit_bias;         /* [E] or NULL                                               */
+  const float* select_bias;        /* [E] or NULL                                               */
+  const void* packed;              /* of mote_router_pack                                       */
+} mote_router_t;
+
+/* What the router kernels want to know of the weights beforehand (the largest norm of a row, for the error bound; the rows
+ * laid out for the tensor cores).  Offline step, once per router; again whenever Wr changes. */
+size_t mote_router_pack_bytes(int E, int64_t d, int w_dtype);       /* 0 if the shape or type is invalid */
+mote_status_t mote_router_pack(const void* Wr, int w_dtype, int E, int64_t d, void* packed, size_t packed_bytes,
+                               void* stream);
+mote_status_t mote_route_scored(const mote_router_t* R, const void* x_bf16, int64_t ldx, int64_t T, int32_t* topk_idx,
+                                float* topk_w, float* logits, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
  * Layer description (Eq. 2-6).  All device pointers, immutable while calls are in flight.
  */
 typedef struct {
@@ -259,6 +306,15 @@ mote_status_t mote_moe_forward(const mote_layer_t* L, const void* x_bf16,
                                const void* residual_bf16, int64_t T, void* out_bf16,
                                const mote_taps_t* taps, void* ws, size_t ws_bytes, void* stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * mote_moe_forward_scored -- mote_moe_forward with the router of mote_route_scored in the place of Eq. 3's: L->Wr,
+ * L->router_bias and L->norm_topk are not used (Wr may be NULL), everything else is as in mote_moe_forward.
+ * Errors: as mote_moe_forward and mote_route_scored; R's d, E or k differ from L's -> ERR_SHAPE.
+ */
+mote_status_t mote_moe_forward_scored(const mote_layer_t* L, const mote_router_t* R, const void* x_bf16,
+                                      const void* residual_bf16, int64_t T, void* out_bf16,
+                                      const mote_taps_t* taps, void* ws, size_t ws_bytes, void* stream);
+
 /* Same layer with HOST input and output: copies x_host (and residual_host if non-NULL) to the
  * device, runs mote_moe_forward, copies the result to out_host and waits for the stream.  Host
  * buffers should be page-locked for the copies to be asynchronous.  Needs
@@ -282,6 +338,72 @@ mote_status_t mote_moe_forward_host(const mote_layer_t* L, const void* x_host,
  * x_bf16, y_bf16: [T, d] bf16 contiguous, 16-B aligned; y may alias x.  Errors: d % 8 != 0 -> ERR_SHAPE.
  */
 mote_status_t mote_rms_norm(const void* x_bf16, int64_t T, int64_t d, float eps, void* y_bf16, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * mote_block_norm -- the norms before and after a block, fused with the block's gate and the residual stream:
+ *
+ *   p  = y, or with post_norm  y * rsqrt( mean_j y[t, j]^2 + eps ) * post_gain[j]
+ *   r' = residual + scale * g * p              g = 1, gate, or 1 / (1 + exp(-gate)) with gate_sigmoid
+ *   n  = bf16( r' * rsqrt( mean_j r'[t, j]^2 + eps ) * pre_gain[j] )
+ *
+ * fp32 arithmetic; r' is rounded once, to the type of the residual stream, and n is the norm of the rounded r' (with unit gain
+ * and no gate: what mote_rms_norm gives for res_out).  Rows are independent and do not depend on T.
+ *
+ *   gate  gate_cols = 0: none.  Else [rows, gate_cols] contiguous of gate_dtype with gate_cols = 1 (one gate for all
+ *         channels) or d, and rows = ceil(T / gate_tokens): gate_tokens consecutive tokens share a row (1: a row for each
+ *         token; the tokens of a sequence: conditioned blocks); gate_tokens = 0: one row for all (a gain for each channel)
+ *   y        in  [T, d] bf16, row stride ldy elements;  residual in [T, d] of res_dtype, row stride ldr elements, or NULL
+ *            (zeros).  Strides >= d, rows on 16-byte boundaries.
+ *   res_out  out [T, d] contiguous of res_dtype, or NULL;  normed_out out [T, d] bf16 contiguous, or NULL; not both NULL
+ * An output may take the place of an input of the same element size and layout; any other overlap of the ranges is refused.
+ * All pointers 16-B aligned but for a gate with gate_cols = 1 (its element's size).
+ * T = 0 is a no-op.  Errors: d % 8 != 0, d > 32768, eps < 0, gate_cols not 0, 1 or d, gate_tokens < 0, overlap -> ERR_SHAPE;
+ * ERR_DTYPE; ERR_NULL; ERR_ALIGN.
+ */
+typedef struct {
+  int32_t d;
+  float eps, scale;
+  int32_t post_norm;               /* 1: y is normalised first                                  */
+  const float* post_gain;          /* [d] or NULL (ones)                                        */
+  const float* pre_gain;           /* [d] or NULL (ones)                                        */
+  int32_t res_dtype;               /* MOTE_DTYPE_*: residual and res_out                        */
+  int32_t gate_cols, gate_dtype, gate_sigmoid;
+  int64_t gate_tokens;
+} mote_block_norm_t;
+mote_status_t mote_block_norm(const mote_block_norm_t* N, const void* y_bf16, int64_t ldy, const void* residual,
+                              int64_t ldr, const void* gate, int64_t T, void* res_out, void* normed_out_bf16,
+                              void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * mote_linear -- matrix product with bias, activation and residual in its epilogue, for the projections beside the
+ * layer:
+ *
+ *   out = act( w_scale[n] * sum_j x[t, j] W[n, j] + bias[n] ) + residual[t, n]
+ *
+ * fp32 accumulation and epilogue, one rounding to the output's type.
+ *   W         [N, K] bf16 (bits = 16 or 0), or the q of mote_rtn_quant with its scale (bits = 8 or 4)
+ *   bias      [N] float or NULL;  act: MOTE_ACT_* (GELU with erf, GELU_TANH its tanh form)
+ *   x_bf16    in  [T, K] bf16, row stride ldx elements (ldx >= K, ldx % 8 == 0)
+ *   residual  in  [T, N] bf16, row stride ldr elements (ldr >= N), or NULL; may be out itself (bf16, ldr = N)
+ *   out       out [T, N] contiguous of out_dtype; must not overlap x
+ *   ws        scratch, >= mote_linear_workspace_bytes(L, T), 256-B aligned; its first word is the device status of
+ *             mote_device_status.  Contents need not be kept between calls; two calls that can run at the same time need two.
+ * Pointers 16-B aligned.  N is arbitrary; K % 8 == 0 (codes: K % 16 == 0).
+ * T = 0 is a no-op.  Errors: N or K out of range (N <= 2^24, K <= 65536), unknown bits or act, overlap -> ERR_SHAPE; ERR_DTYPE;
+ * ERR_NULL; ERR_ALIGN; ERR_WORKSPACE.
+ */
+enum { MOTE_ACT_NONE = 0, MOTE_ACT_RELU = 1, MOTE_ACT_SILU = 2, MOTE_ACT_GELU = 3, MOTE_ACT_GELU_TANH = 4 };
+typedef struct {
+  int64_t N, K;
+  const void* W;
+  int32_t bits;                    /* 16 (or 0), 8, 4: as shared_bits of mote_layer_t           */
+  const float* w_scale;            /* [N] for codes; ignored for bf16                           */
+  const float* bias;
+  int32_t act;
+} mote_linear_t;
+size_t mote_linear_workspace_bytes(const mote_linear_t* L, int64_t T_max);    /* 0 if the shape is invalid */
+mote_status_t mote_linear(const mote_linear_t* L, const void* x_bf16, int64_t ldx, int64_t T, const void* residual_bf16,
+                          int64_t ldr, void* out, int out_dtype, void* ws, size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------------------------------
  * mote_stack_forward -- n_layers MoTE FFN layers back to back as Eq. 1-2 chain them (the attention

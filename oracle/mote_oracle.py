@@ -401,12 +401,93 @@ def rms_norm(x_bf16: np.ndarray, eps: float) -> np.ndarray:
 
 
 # --------------------------------------------------------------------------------------------
+# The operators around the experts: scored router, norms around a block, projections
+# --------------------------------------------------------------------------------------------
+
+
+def route_scored(x: np.ndarray, Wr: np.ndarray, k: int, *, scoring="softmax", logit_bias=None, select_bias=None, n_groups=1,
+                 topk_groups=1, renorm=True, scale=1.0):
+    """Router with softmax or sigmoid scores, a bias that takes part in the choice alone, groups and renormalised weights, fp64,
+    token by token.  x [T, d] and Wr [E, d] as fp64 values of the stored ones.  Without select_bias and groups the experts are
+    ordered by logit (scores grow with it), else by c = score + select_bias; a tie goes to the lower index."""
+    T, E = x.shape[0], Wr.shape[0]
+    l = x.astype(np.float64) @ Wr.astype(np.float64).T
+    if logit_bias is not None:
+        l = l + np.asarray(logit_bias, np.float64)
+    idx, w = np.zeros((T, k), np.int32), np.zeros((T, k))
+    per = E // n_groups
+    for t in range(T):
+        if scoring == "softmax":
+            e = np.exp(l[t] - l[t].max())
+            s = e / e.sum()
+        else:
+            with np.errstate(over="ignore"):
+                s = 1.0 / (1.0 + np.exp(-l[t]))
+        c = l[t] if select_bias is None and n_groups == 1 else s
+        if select_bias is not None:
+            c = c + np.asarray(select_bias, np.float64)
+        group = [sum(sorted(c[g * per:(g + 1) * per], reverse=True)[:2]) for g in range(n_groups)]
+        kept = sorted(range(n_groups), key=lambda g: (-group[g], g))[:topk_groups]
+        open_ = [e for e in range(E) if e // per in kept]
+        pick = sorted(open_, key=lambda e: (-c[e], e))[:k]
+        idx[t] = pick
+        w[t] = scale * s[pick] / (max(s[pick].sum(), 1e-20) if renorm else 1.0)
+    return dict(logits=l, idx=idx, w=w, near_tie=np.zeros(T, dtype=bool))
+
+
+def block_norm(y, residual, *, eps, scale=1.0, post_norm=False, post_gain=None, gate=None, gate_sigmoid=False, gate_tokens=1):
+    """r' = residual + scale * g * p of the norms around a block, fp64, not rounded.  gate [rows, 1 or d] or None."""
+    p = np.asarray(y, np.float64)
+    if post_norm:
+        p = p / np.sqrt(np.mean(p * p, axis=1, keepdims=True) + eps)
+        if post_gain is not None:
+            p = p * np.asarray(post_gain, np.float64)
+    if gate is not None:
+        g = np.asarray(gate, np.float64)
+        if gate_sigmoid:
+            g = 1.0 / (1.0 + np.exp(-g))
+        t = np.arange(p.shape[0])
+        p = p * g[t // gate_tokens if gate_tokens else 0 * t]
+    return (0.0 if residual is None else np.asarray(residual, np.float64)) + scale * p
+
+
+def gained_rms_norm(r, gain, eps):
+    """The norm before the next block, of the stored residual stream; fp64, not rounded."""
+    r = np.asarray(r, np.float64)
+    n = r / np.sqrt(np.mean(r * r, axis=1, keepdims=True) + eps)
+    return n if gain is None else n * np.asarray(gain, np.float64)
+
+
+def activation(z: np.ndarray, act: str) -> np.ndarray:
+    from math import erf
+    if act == "relu":
+        return np.maximum(z, 0.0)
+    with np.errstate(over="ignore"):
+        if act == "silu":
+            return z / (1.0 + np.exp(-z))
+        if act == "gelu":
+            return 0.5 * z * (1.0 + np.vectorize(erf, otypes=[np.float64])(z / np.sqrt(2.0)))
+        if act == "gelu_tanh":
+            return 0.5 * z * (1.0 + np.tanh(np.sqrt(2.0 / np.pi) * (z + 0.044715 * z ** 3)))
+    return z
+
+
+def linear(x, W, *, bias=None, act="none", residual=None):
+    """act(x W^T + bias) + residual in fp64; W [N, K] are the dequantized weights."""
+    z = np.asarray(x, np.float64) @ np.asarray(W, np.float64).T
+    if bias is not None:
+        z = z + np.asarray(bias, np.float64)
+    z = activation(z, act)
+    return z if residual is None else z + np.asarray(residual, np.float64)
+
+
+# --------------------------------------------------------------------------------------------
 # Eq. 2, 4  the whole layer
 # --------------------------------------------------------------------------------------------
 
 
 def moe_forward(layer: dict, x_bf16: np.ndarray, residual_bf16=None, token_subset=None,
-                near_tie_choice=None):
+                near_tie_choice=None, route=None):
     """out = [residual +] FFN(x) + sum_j w_j * FFN^T_{e_j}(x)   (Eq. 2 and Eq. 4).
 
     layer: dict with d, f, E, k, norm_topk, Wr[E,d] f32, router_bias[E] f32 or None,
@@ -422,10 +503,11 @@ def moe_forward(layer: dict, x_bf16: np.ndarray, residual_bf16=None, token_subse
       and (k+1)-th logit closer than 1e-5, where an fp32 router may legitimately pick the other
       expert) the selection is taken from this array instead, and the gate weights are
       recomputed from the oracle's own logits; every other token keeps the oracle's selection.
+    route: optional routing (the dict of route_scored) in the place of Eq. 3's.
     Returns a dict of every intermediate named after the stages above."""
     E, k = layer["E"], layer["k"]
     T, d = x_bf16.shape
-    r = router(x_bf16, layer["Wr"], layer.get("router_bias"), k, layer["norm_topk"])
+    r = route if route is not None else router(x_bf16, layer["Wr"], layer.get("router_bias"), k, layer["norm_topk"])
     if near_tie_choice is not None and r["near_tie"].any():
         for t in np.nonzero(r["near_tie"])[0]:
             sel_idx = np.asarray(near_tie_choice[t], dtype=np.int32)

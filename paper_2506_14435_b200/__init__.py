@@ -5,6 +5,7 @@ name below and fails loudly if the library has not been built
 
 _EXPORTS = ["MoteError", "MoteLayer", "lib", "mote_ternarize_pack", "mote_ternarize_pack_static", "mote_rtn_quant", "mote_quant_act", "mote_route_topk", "mote_route_stats",
             "mote_moe_forward", "mote_moe_forward_host", "MoteStack", "mote_stack_forward", "mote_rms_norm", "mote_moe_forward_profile", "PATH_AUTO", "PATH_SIMT",
+            "MoteRouter", "mote_route_scored", "mote_moe_forward_scored", "MoteBlockNorm", "mote_block_norm", "MoteLinear", "mote_linear", "ACTS",
             "PATH_TENSOR", "PATH_STREAM", "STAGE_NAMES"]
 __all__ = list(_EXPORTS)
 

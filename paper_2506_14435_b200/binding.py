@@ -32,6 +32,23 @@ class mote_layer_t(C.Structure):
 _LAYER_POINTERS = [n for n, t in mote_layer_t._fields_ if t is C.c_void_p]   # 11 ahead of shared_bits, 3 behind
 
 
+class mote_router_t(C.Structure):
+    _fields_ = [("d", C.c_int32), ("E", C.c_int32), ("k", C.c_int32), ("scoring", C.c_int32), ("n_groups", C.c_int32),
+                ("topk_groups", C.c_int32), ("renorm", C.c_int32), ("scale", C.c_float), ("Wr", C.c_void_p),
+                ("w_dtype", C.c_int32), ("logit_bias", C.c_void_p), ("select_bias", C.c_void_p), ("packed", C.c_void_p)]
+
+
+class mote_block_norm_t(C.Structure):
+    _fields_ = [("d", C.c_int32), ("eps", C.c_float), ("scale", C.c_float), ("post_norm", C.c_int32),
+                ("post_gain", C.c_void_p), ("pre_gain", C.c_void_p), ("res_dtype", C.c_int32), ("gate_cols", C.c_int32),
+                ("gate_dtype", C.c_int32), ("gate_sigmoid", C.c_int32), ("gate_tokens", C.c_int64)]
+
+
+class mote_linear_t(C.Structure):
+    _fields_ = [("N", C.c_int64), ("K", C.c_int64), ("W", C.c_void_p), ("bits", C.c_int32), ("w_scale", C.c_void_p),
+                ("bias", C.c_void_p), ("act", C.c_int32)]
+
+
 TAP_FIELDS = ["topk_idx", "topk_w", "offsets", "perm", "qx", "beta_x", "acc_gate", "acc_up", "h_bf16",
               "qh", "beta_h", "acc_down", "y", "shared_out"]
 
@@ -69,6 +86,24 @@ lib.mote_host_staging_bytes.argtypes = [C.c_int, C.c_int64]
 lib.mote_moe_forward.restype = C.c_int
 lib.mote_moe_forward.argtypes = [C.POINTER(mote_layer_t), C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p,
                                  C.POINTER(mote_taps_t), C.c_void_p, C.c_size_t, C.c_void_p]
+lib.mote_router_pack_bytes.restype = C.c_size_t
+lib.mote_router_pack_bytes.argtypes = [C.c_int, C.c_int64, C.c_int]
+lib.mote_router_pack.restype = C.c_int
+lib.mote_router_pack.argtypes = [C.c_void_p, C.c_int, C.c_int, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]
+lib.mote_route_scored.restype = C.c_int
+lib.mote_route_scored.argtypes = [C.POINTER(mote_router_t), C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p,
+                                  C.c_void_p]
+lib.mote_moe_forward_scored.restype = C.c_int
+lib.mote_moe_forward_scored.argtypes = [C.POINTER(mote_layer_t), C.POINTER(mote_router_t), C.c_void_p, C.c_void_p, C.c_int64,
+                                        C.c_void_p, C.POINTER(mote_taps_t), C.c_void_p, C.c_size_t, C.c_void_p]
+lib.mote_block_norm.restype = C.c_int
+lib.mote_block_norm.argtypes = [C.POINTER(mote_block_norm_t), C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
+                                C.c_void_p, C.c_void_p, C.c_void_p]
+lib.mote_linear_workspace_bytes.restype = C.c_size_t
+lib.mote_linear_workspace_bytes.argtypes = [C.POINTER(mote_linear_t), C.c_int64]
+lib.mote_linear.restype = C.c_int
+lib.mote_linear.argtypes = [C.POINTER(mote_linear_t), C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int,
+                            C.c_void_p, C.c_size_t, C.c_void_p]
 lib.mote_stack_workspace_bytes.restype = C.c_size_t
 lib.mote_stack_workspace_bytes.argtypes = [C.POINTER(mote_layer_t), C.c_int, C.c_int64]
 lib.mote_stack_forward.restype = C.c_int
@@ -202,6 +237,195 @@ def mote_route_stats(logits: torch.Tensor, topk_idx: torch.Tensor):
     return cnt, ps
 
 
+_DTYPES = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16}
+
+
+def _here(dev: int):
+    # the library works on the current device and stream
+    if dev != torch.cuda.current_device():
+        raise ValueError("expected tensors on the current CUDA device")
+
+
+def _rows(t: torch.Tensor, name: str, dtype, shape, dev: int) -> int:
+    """Row stride of a [rows, cols] CUDA matrix with unit inner stride."""
+    if t.dtype is not dtype or t.get_device() != dev or tuple(t.shape) != shape or (t.stride(1) != 1 and shape[1] > 1):
+        raise ValueError(f"{name}: expected {dtype} {list(shape)} with unit inner stride on cuda:{dev}")
+    return t.stride(0) if shape[0] > 1 else shape[1]
+
+
+def _vector(t, name: str, n: int, dev):
+    """An optional [n] float32 weight, and its address."""
+    if t is None:
+        return None, None
+    if t.dtype is not torch.float32 or not t.is_cuda or tuple(t.shape) != (n,) or (dev is not None and t.get_device() != dev):
+        raise ValueError(f"{name}: expected float32 [{n}] on the device of the weights")
+    t = t.contiguous()
+    return t, t.data_ptr()
+
+
+class MoteRouter:
+    """A scored router's weights and options (mote_router_t): Wr[E, d] fp32 or bf16; scoring "softmax" or "sigmoid"; logit_bias and
+    select_bias[E] fp32.  Construction runs mote_router_pack; make a new one when Wr has changed."""
+
+    def __init__(self, Wr, k, scoring="softmax", logit_bias=None, select_bias=None, n_groups=1, topk_groups=1, renorm=True, scale=1.0):
+        _need_cuda(Wr)
+        if Wr.dim() != 2 or Wr.dtype not in _DTYPES:
+            raise ValueError("Wr: expected a float32 or bfloat16 matrix")
+        self.E, self.d = Wr.shape
+        self.k = k
+        self.device = Wr.get_device()
+        _here(self.device)
+        lb, lb_ptr = _vector(logit_bias, "logit_bias", self.E, self.device)
+        sb, sb_ptr = _vector(select_bias, "select_bias", self.E, self.device)
+        dt = _DTYPES[Wr.dtype]
+        need = lib.mote_router_pack_bytes(self.E, self.d, dt)
+        if need == 0:
+            raise MoteError(2, "mote_router_pack_bytes")
+        packed = torch.empty(need, dtype=torch.uint8, device=Wr.device)
+        _check(lib.mote_router_pack(_ptr(Wr), dt, self.E, self.d, _ptr(packed), need, _stream()), "mote_router_pack")
+        self.tensors = dict(Wr=Wr, logit_bias=lb, select_bias=sb, packed=packed)
+        self.struct = mote_router_t(self.d, self.E, k, {"softmax": 0, "sigmoid": 1}[scoring], n_groups, topk_groups, int(renorm), scale,
+                                    Wr.data_ptr(), dt, lb_ptr, sb_ptr, packed.data_ptr())
+        self._ref = C.byref(self.struct)
+
+
+def mote_route_scored(router: MoteRouter, x: torch.Tensor, want_logits: bool = False):
+    """x[T, d] bf16 (rows may be strided) -> (topk_idx int32[T, k], topk_w f32[T, k], logits f32[T, E] or None)."""
+    T = x.shape[0]
+    dev = router.device
+    _here(dev)
+    ldx = _rows(x, "x", torch.bfloat16, (T, router.d), dev)
+    idx = torch.empty((T, router.k), dtype=torch.int32, device=x.device)
+    w = torch.empty((T, router.k), dtype=torch.float32, device=x.device)
+    logits = torch.empty((T, router.E), dtype=torch.float32, device=x.device) if want_logits else None
+    _check(lib.mote_route_scored(router._ref, x.data_ptr(), ldx, T, idx.data_ptr(), w.data_ptr(),
+                                 logits.data_ptr() if want_logits else None, _stream()), "mote_route_scored")
+    return idx, w, logits
+
+
+class MoteBlockNorm:
+    """The norms around a block (mote_block_norm_t): post_gain, pre_gain [d] fp32 or None; gate_tokens: consecutive tokens that share
+    a row of the gate (1: a row each, 0: one row for all)."""
+
+    def __init__(self, d, eps=1e-6, post_norm=False, post_gain=None, pre_gain=None, scale=1.0, gate_sigmoid=False, gate_tokens=1):
+        self.d, self.gate_tokens = d, gate_tokens
+        pg, pg_ptr = _vector(post_gain, "post_gain", d, None)
+        ng, ng_ptr = _vector(pre_gain, "pre_gain", d, pg.get_device() if pg is not None else None)
+        self.device = pg.get_device() if pg is not None else ng.get_device() if ng is not None else None
+        self.tensors = dict(post_gain=pg, pre_gain=ng)
+        # residual type, columns and type of the gate: (1, 0, 0) and the like, filled in by the call
+        self._args = (d, eps, scale, int(post_norm), pg_ptr, ng_ptr), (int(gate_sigmoid), gate_tokens)
+        self._structs = {}
+
+    def struct(self, res_dtype: int, gate_cols: int, gate_dtype: int):
+        key = (res_dtype, gate_cols, gate_dtype)
+        ref = self._structs.get(key)
+        if ref is None:
+            ref = self._structs[key] = C.byref(mote_block_norm_t(*self._args[0], *key, *self._args[1]))
+        return ref
+
+
+def mote_block_norm(norm: MoteBlockNorm, y: torch.Tensor, residual=None, gate=None, res_out=None, normed_out=None,
+                    want_residual: bool = True, want_normed: bool = True):
+    """y[T, d] bf16 -> (res_out [T, d] of the residual's type, normed_out [T, d] bf16); either is None where not wanted.  gate:
+    [rows, 1] or [rows, d], bf16 or fp32, with rows = ceil(T / gate_tokens).  res_out may be residual, normed_out may be y."""
+    d = norm.d
+    T = y.shape[0]
+    dev = y.get_device()
+    _here(dev)
+    if norm.device is not None and norm.device != dev:
+        raise ValueError("the gains are on another device")
+    ldy = _rows(y, "y", torch.bfloat16, (T, d), dev)
+    res_dtype = torch.bfloat16
+    if residual is not None:
+        res_dtype = residual.dtype
+    elif res_out is not None:
+        res_dtype = res_out.dtype
+    if res_dtype not in _DTYPES:
+        raise ValueError("residual: expected float32 or bfloat16")
+    ldr = _rows(residual, "residual", res_dtype, (T, d), dev) if residual is not None else d
+    cols, gate_dt = 0, 0
+    if gate is not None:
+        rows = min(T, 1) if norm.gate_tokens == 0 else -(-T // norm.gate_tokens)
+        cols = gate.shape[1] if gate.dim() == 2 else -1
+        if cols not in (1, d) or gate.shape[0] != rows or gate.dtype not in _DTYPES or not gate.is_contiguous() or gate.get_device() != dev:
+            raise ValueError(f"gate: expected contiguous float32 or bfloat16 [{rows}, 1] or [{rows}, {d}]")
+        gate_dt = _DTYPES[gate.dtype]
+    for name, o, dt in (("res_out", res_out, res_dtype), ("normed_out", normed_out, torch.bfloat16)):
+        if o is not None and (_rows(o, name, dt, (T, d), dev) != d):
+            raise ValueError(f"{name}: expected contiguous rows")
+    if res_out is None and want_residual:
+        res_out = torch.empty((T, d), dtype=res_dtype, device=y.device)
+    if normed_out is None and want_normed:
+        normed_out = torch.empty((T, d), dtype=torch.bfloat16, device=y.device)
+    _check(lib.mote_block_norm(norm.struct(_DTYPES[res_dtype], cols, gate_dt), y.data_ptr(), ldy,
+                               None if residual is None else residual.data_ptr(), ldr, None if gate is None else gate.data_ptr(), T,
+                               None if res_out is None else res_out.data_ptr(), None if normed_out is None else normed_out.data_ptr(),
+                               _stream()), "mote_block_norm")
+    return res_out, normed_out
+
+
+ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}
+
+
+class MoteLinear:
+    """A projection's weights (mote_linear_t): W[N, K] bf16, or the codes of mote_rtn_quant (bits 8: int8[N, K], bits 4:
+    uint8[N, K / 2]) with scale[N] fp32; bias[N] fp32 or None; act one of ACTS."""
+
+    def __init__(self, W, bits=16, scale=None, bias=None, act="none"):
+        _need_cuda(W)
+        if bits not in (16, 8, 4) or W.dim() != 2 or W.dtype is not {16: torch.bfloat16, 8: torch.int8, 4: torch.uint8}[bits]:
+            raise ValueError("W: expected bfloat16 [N, K] (bits 16), int8 [N, K] (8) or uint8 [N, K / 2] (4)")
+        if act not in ACTS:
+            raise ValueError(f"act: expected one of {sorted(ACTS)}")
+        if (scale is None) != (bits == 16):
+            raise ValueError("scale: expected with codes, and with codes only")
+        self.N, self.K, self.bits = W.shape[0], W.shape[1] * (2 if bits == 4 else 1), bits
+        self.device = W.get_device()
+        sc, sc_ptr = _vector(scale, "scale", self.N, self.device)
+        b, b_ptr = _vector(bias, "bias", self.N, self.device)
+        self.tensors = dict(W=W, scale=sc, bias=b)
+        self.struct = mote_linear_t(self.N, self.K, W.data_ptr(), bits, sc_ptr, b_ptr, ACTS[act])
+        self._ref = C.byref(self.struct)
+        self._ws = None
+        self._ws_T = -1                      # the workspace serves up to this many tokens
+
+    @classmethod
+    def quantized(cls, W, bits, bias=None, act="none"):
+        """Offline step: RTN codes of W[N, K] (fp32 or bf16) by mote_rtn_quant."""
+        q, scale = mote_rtn_quant(W, bits)
+        return cls(q, bits=bits, scale=scale, bias=bias, act=act)
+
+    def workspace(self, T: int) -> torch.Tensor:
+        if T > self._ws_T:
+            need = lib.mote_linear_workspace_bytes(self._ref, T)
+            if need == 0:
+                raise MoteError(2, "mote_linear_workspace_bytes")
+            if self._ws is None or self._ws.numel() < need:
+                self._ws = torch.empty(need, dtype=torch.uint8, device=self.tensors["W"].device)
+            self._ws_T = T
+        return self._ws
+
+
+def mote_linear(linear: MoteLinear, x: torch.Tensor, residual=None, out=None, out_dtype=torch.bfloat16):
+    """x[T, K] bf16 (rows may be strided) -> act(x W^T + bias) + residual, [T, N] of out_dtype (or out's type); out may be
+    residual.  Uses the layer's own workspace: calls of one MoteLinear that can run at the same time need one object each."""
+    T, dev = x.shape[0], linear.device
+    _here(dev)
+    ldx = _rows(x, "x", torch.bfloat16, (T, linear.K), dev)
+    ldr = _rows(residual, "residual", torch.bfloat16, (T, linear.N), dev) if residual is not None else linear.N
+    if out is None:
+        out = torch.empty((T, linear.N), dtype=out_dtype, device=x.device)
+    elif out.dtype not in _DTYPES or _rows(out, "out", out.dtype, (T, linear.N), dev) != linear.N:
+        raise ValueError("out: expected contiguous float32 or bfloat16 rows")
+    if out.dtype not in _DTYPES:
+        raise ValueError("out_dtype: expected float32 or bfloat16")
+    ws = linear.workspace(T)
+    _check(lib.mote_linear(linear._ref, x.data_ptr(), ldx, T, None if residual is None else residual.data_ptr(), ldr, out.data_ptr(),
+                           _DTYPES[out.dtype], ws.data_ptr(), ws.numel(), _stream()), "mote_linear")
+    return out
+
+
 class MoteLayer:
     """Device-resident weights of one MoTE layer plus its mote_layer_t."""
 
@@ -318,6 +542,26 @@ def mote_moe_forward(layer: MoteLayer, x: torch.Tensor, residual=None, out=None,
         tp = C.byref(tp)
     _check(lib.mote_moe_forward(C.byref(s), _ptr(x), _ptr(residual), T, _ptr(out), tp, _ptr(ws), ws.numel(),
                                 _stream()), "mote_moe_forward")
+    return out
+
+
+def mote_moe_forward_scored(layer: MoteLayer, router: MoteRouter, x: torch.Tensor, residual=None, out=None, taps: dict | None = None):
+    """mote_moe_forward with `router` (mote_route_scored) in the place of the layer's own."""
+    _need_cuda(x, residual, out)
+    _here(router.device)
+    T = x.shape[0]
+    if out is None:
+        out = torch.empty_like(x)
+    s = layer.struct()
+    ws = layer.workspace(T, struct=s)
+    tp = None
+    if taps is not None:
+        tp = mote_taps_t()
+        for n, t in taps.items():
+            setattr(tp, n, t.data_ptr())
+        tp = C.byref(tp)
+    _check(lib.mote_moe_forward_scored(C.byref(s), router._ref, _ptr(x), _ptr(residual), T, _ptr(out), tp, _ptr(ws), ws.numel(),
+                                       _stream()), "mote_moe_forward_scored")
     return out
 
 

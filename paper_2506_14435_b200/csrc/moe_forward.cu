@@ -232,9 +232,9 @@ extern "C" mote_status_t mote_selftest_bounded_wait(void* ws, uint64_t limit_ns,
   return launch_bounded_wait_selftest(static_cast<uint32_t*>(ws), limit_ns, static_cast<cudaStream_t>(stream_));
 }
 
-extern "C" mote_status_t mote_moe_forward(const mote_layer_t* L, const void* x, const void* residual, int64_t T,
-                                          void* out, const mote_taps_t* taps, void* ws, size_t ws_bytes,
-                                          void* stream_) {
+// R: the scored router that takes the place of Eq. 3's, or null
+static mote_status_t layer_forward(const mote_layer_t* L, const mote_router_t* R, const void* x, const void* residual, int64_t T,
+                                   void* out, const mote_taps_t* taps, void* ws, size_t ws_bytes, void* stream_) {
   g_launch_count = 0;
   for (int& tile : g_gemm_tile) tile = 0;
   if (!L) return MOTE_ERR_NULL;
@@ -242,7 +242,7 @@ extern "C" mote_status_t mote_moe_forward(const mote_layer_t* L, const void* x, 
   if (!shape_ok(d, f, E, k) || T < 0 || T > (int64_t(1) << 24)) return MOTE_ERR_SHAPE;
   if (L->path < MOTE_PATH_AUTO || L->path > MOTE_PATH_STREAM) return MOTE_ERR_SHAPE;
   if (T == 0) return MOTE_OK;
-  if (!x || !out || !ws || !L->Wr || !L->gate_packed || !L->up_packed || !L->down_packed || !L->alpha_gate ||
+  if (!x || !out || !ws || (!R && !L->Wr) || !L->gate_packed || !L->up_packed || !L->down_packed || !L->alpha_gate ||
       !L->alpha_up || !L->alpha_down || !L->sh_gate || !L->sh_up || !L->sh_down)
     return MOTE_ERR_NULL;
   if (x == out) return MOTE_ERR_SHAPE;
@@ -253,7 +253,7 @@ extern "C" mote_status_t mote_moe_forward(const mote_layer_t* L, const void* x, 
   const SharedMat sh_gate{L->sh_gate, sh_rtn ? L->sh_gate_scale : nullptr};
   const SharedMat sh_up{L->sh_up, sh_rtn ? L->sh_up_scale : nullptr};
   const SharedMat sh_down{L->sh_down, sh_rtn ? L->sh_down_scale : nullptr};
-  const void* ptrs[] = {x, out, residual, L->Wr, L->gate_packed, L->up_packed, L->down_packed,
+  const void* ptrs[] = {x, out, residual, R ? nullptr : L->Wr, L->gate_packed, L->up_packed, L->down_packed,
                         L->sh_gate, L->sh_up, L->sh_down, sh_gate.scale, sh_up.scale, sh_down.scale};
   for (const void* p : ptrs)
     if (p && !aligned16(p)) return MOTE_ERR_ALIGN;
@@ -301,7 +301,7 @@ extern "C" mote_status_t mote_moe_forward(const mote_layer_t* L, const void* x, 
     // status word, the prologue's arrival counter, the down kernel's tile counters
     // (the kernels leave their counters at zero, so inside a stack the stack's one memset is enough)
     // (a single-token call lets its prologue kernel do it: one operation less on the stream)
-    const bool prologue_zeroes = !g_keep_status && T == 1;
+    const bool prologue_zeroes = !g_keep_status && T == 1 && !R;
     if (!g_keep_status && !prologue_zeroes) MOTE_CUDA_OK(cudaMemsetAsync(status, 0, status_region_bytes(d), stream));
     stage_mark(0, stream);
     DecodeStreamArgs ds{};
@@ -318,8 +318,22 @@ extern "C" mote_status_t mote_moe_forward(const mote_layer_t* L, const void* x, 
     ds.tap_gate = taps ? taps->acc_gate : nullptr; ds.tap_up = taps ? taps->acc_up : nullptr;
     ds.tap_down = taps ? taps->acc_down : nullptr;
     if (taps && (!taps->acc_gate != !taps->acc_up)) return MOTE_ERR_NULL;
-    mote_status_t st = launch_decode_stream(ds, 0, stream);   // Q_a(x), router, dispatch in one kernel
-    if (st) return st;
+    mote_status_t st;
+    if (R) {                                                  // what the prologue kernel does, step by step
+      st = launch_route_scored(R, x, d, T, topk_idx, topk_w, nullptr, stream);
+      if (st) return st;
+      st = launch_dispatch(topk_idx, P, E, offsets, perm, inv, stream);
+      if (st) return st;
+      QuantActArgs qa{};
+      qa.x = x; qa.T = T; qa.d = d; qa.ldx = d; qa.q = qx; qa.beta = beta_x; qa.rowsum = rowsum_x; qa.k = 1; qa.interleave = 1;
+      st = launch_quant_act(qa, false, stream);
+      if (st) return st;
+      MOTE_CUDA_OK(cudaMemsetAsync(beta_h, 0, P * 4, stream));
+      MOTE_CUDA_OK(cudaMemsetAsync(rowsum_h, 0, P * 4, stream));
+    } else {
+      st = launch_decode_stream(ds, 0, stream);               // Q_a(x), router, dispatch in one kernel
+      if (st) return st;
+    }
     stage_mark(1, stream); stage_mark(2, stream); stage_mark(3, stream);
     st = launch_decode_stream(ds, 1, stream);                 // routed and shared gate/up
     if (st) return st;
@@ -374,7 +388,7 @@ extern "C" mote_status_t mote_moe_forward(const mote_layer_t* L, const void* x, 
   mote_status_t st;
   // device status word: cleared by the router kernel where the tensor-core router runs (one
   // operation less on the stream), else by a memset
-  const bool router_clears = !g_keep_status && tensor;
+  const bool router_clears = !g_keep_status && tensor && !R;
   if (!g_keep_status && !router_clears) MOTE_CUDA_OK(cudaMemsetAsync(status, 0, 4, stream));
   stage_mark(0, stream);
   // S1 router, S2 dispatch
@@ -383,8 +397,13 @@ extern "C" mote_status_t mote_moe_forward(const mote_layer_t* L, const void* x, 
   auto* blk_hist = reinterpret_cast<int32_t*>(base + pl.blk_hist);
   auto* blk_base = reinterpret_cast<int32_t*>(base + pl.blk_base);
   const int n_blk = (int)((T + kRouteBlockTokens - 1) / kRouteBlockTokens);
-  st = launch_route_topk(x, T, d, L->Wr, L->router_bias, E, k, L->norm_topk, topk_idx, topk_w, nullptr,
-                         tensor ? blk_hist : nullptr, stream, router_clears ? status : nullptr);
+  if (R) {
+    st = launch_route_scored(R, x, d, T, topk_idx, topk_w, nullptr, stream);
+    if (!st && tensor) st = launch_block_counts(topk_idx, T, E, k, blk_hist, stream);
+  } else {
+    st = launch_route_topk(x, T, d, L->Wr, L->router_bias, E, k, L->norm_topk, topk_idx, topk_w, nullptr,
+                           tensor ? blk_hist : nullptr, stream, router_clears ? status : nullptr);
+  }
   if (st) return st;
   stage_mark(1, stream);
   const bool inline_scan = tensor && n_blk <= kInlineScanBlocks;   // few blocks: done by the CTAs of Q_a(x)
@@ -526,6 +545,23 @@ extern "C" mote_status_t mote_moe_forward(const mote_layer_t* L, const void* x, 
     }
   }
   return MOTE_OK;
+}
+
+extern "C" mote_status_t mote_moe_forward(const mote_layer_t* L, const void* x, const void* residual, int64_t T,
+                                          void* out, const mote_taps_t* taps, void* ws, size_t ws_bytes,
+                                          void* stream_) {
+  return layer_forward(L, nullptr, x, residual, T, out, taps, ws, ws_bytes, stream_);
+}
+
+extern "C" mote_status_t mote_moe_forward_scored(const mote_layer_t* L, const mote_router_t* R, const void* x, const void* residual,
+                                                 int64_t T, void* out, const mote_taps_t* taps, void* ws, size_t ws_bytes,
+                                                 void* stream_) {
+  g_launch_count = 0;
+  if (!L) return MOTE_ERR_NULL;
+  const mote_status_t st = check_router(R);
+  if (st) return st;
+  if (R->d != L->d || R->E != L->E || R->k != L->k) return MOTE_ERR_SHAPE;
+  return layer_forward(L, R, x, residual, T, out, taps, ws, ws_bytes, stream_);
 }
 
 extern "C" size_t mote_stack_workspace_bytes(const mote_layer_t* layers, int n_layers, int64_t T_max) {

@@ -46,6 +46,13 @@ mote_status_t launch_route_topk(const void* x, int64_t T, int d, const float* Wr
                                 int32_t* blk_hist, cudaStream_t stream, uint32_t* zero_word = nullptr);
 // zero_word (optional, tensor-core kernel only): a word the kernel's first thread sets to zero.
 
+// Scored router (mote_route_scored); check_router: the argument checks of the calls that take one.
+mote_status_t check_router(const mote_router_t* R);
+mote_status_t launch_route_scored(const mote_router_t* R, const void* x, int64_t ldx, int64_t T, int32_t* idx, float* w,
+                                  float* logits, cudaStream_t stream);
+// blk_hist of launch_route_topk from finished choices.
+mote_status_t launch_block_counts(const int32_t* idx, int64_t T, int E, int k, int32_t* blk_hist, cudaStream_t stream);
+
 // Stable grouping of the T*k pairs by expert: offsets[E+1], perm[P] (pair -> row), inv[P] (row -> pair).
 mote_status_t launch_dispatch(const int32_t* idx, int64_t P, int E, int32_t* offsets, int32_t* perm,
                               int32_t* inv, cudaStream_t stream);
