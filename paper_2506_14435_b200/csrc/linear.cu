@@ -8,34 +8,11 @@
 // Up to kStreamMaxTokens tokens the product is a weight stream: a CTA owns 16 rows of W, its warps share K, a lane loads 16 bytes of
 // one weight row straight into registers (codes are expanded there) and feeds them to warp-level MMAs as the A operand with the
 // tokens as the 8-wide B operand.  Every weight byte is read once.
-#include "mote_common.cuh"
-#include "mote_internal.h"
+#include <algorithm>
+
+#include "linear_act.cuh"
 
 namespace mote {
-
-struct LinearArgs {
-  const uint16_t* x; int64_t ldx, T;
-  const void* W; const float* w_scale; const float* bias;
-  const uint16_t* res; int64_t ldr;
-  void* out;
-  int64_t N;
-  int K, act, out_f32;
-  uint32_t* status;                              // device status word, cleared by every call
-};
-
-__device__ __forceinline__ float apply_act(float z, int act) {
-  switch (act) {
-    case MOTE_ACT_RELU: return fmaxf(z, 0.0f);
-    case MOTE_ACT_SILU: return z / (1.0f + expf(-z));
-    case MOTE_ACT_GELU: return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
-    case MOTE_ACT_GELU_TANH: {
-      // 0.5 z (1 + tanh u) = z / (1 + exp(-2u)),  u = sqrt(2/pi) (z + 0.044715 z^3)
-      const float u = 0.79788456080286536f * (z + 0.044715f * z * z * z);
-      return z / (1.0f + expf(-2.0f * u));
-    }
-  }
-  return z;
-}
 
 __device__ __forceinline__ uint4 ldg_once(const void* p) {
   uint4 v;
@@ -176,6 +153,28 @@ static cudaError_t launch_stream(const LinearArgs& a, int bits, cudaStream_t str
                      : launch_pdl(linear_stream_kernel<NT, 4>, grid, block, 0, stream, a);
 }
 
+// RTN codes -> the same integers as bf16, for the tensor-core product; 8 code bytes per thread and step.
+__global__ void __launch_bounds__(256) linear_expand_kernel(const uint2* __restrict__ codes, uint4* __restrict__ out, int64_t n_chunks, int bits) {
+  pdl_wait();
+  const int64_t stride = int64_t(gridDim.x) * blockDim.x;
+  for (int64_t i = int64_t(blockIdx.x) * blockDim.x + threadIdx.x; i < n_chunks; i += stride) {
+    const uint2 w = codes[i];
+    uint32_t e[4], h[4];
+    if (bits == 8) {
+      s8x4_to_bf16x2(w.x, e[0], e[1]);
+      s8x4_to_bf16x2(w.y, e[2], e[3]);
+      out[i] = make_uint4(e[0], e[1], e[2], e[3]);
+    } else {
+      u4x8_to_bf16x2(w.x, e);
+      u4x8_to_bf16x2(w.y, h);
+      out[2 * i] = make_uint4(e[0], e[1], e[2], e[3]);
+      out[2 * i + 1] = make_uint4(h[0], h[1], h[2], h[3]);
+    }
+  }
+}
+
+constexpr int64_t kStreamMaxTokens = 16;
+
 static int linear_bits(const mote_linear_t* L) { return L->bits == 0 ? MOTE_SHARED_BF16 : L->bits; }
 static bool linear_shape_ok(const mote_linear_t* L) {
   const int bits = linear_bits(L);
@@ -192,7 +191,9 @@ static bool ranges_overlap(const void* a, size_t na, const void* b, size_t nb) {
 extern "C" size_t mote_linear_workspace_bytes(const mote_linear_t* L, int64_t T_max) {
   using namespace mote;
   if (!L || !linear_shape_ok(L) || T_max < 0 || T_max > (int64_t(1) << 24)) return 0;
-  return 256;
+  // status word; from kStreamMaxTokens on the codes as bf16
+  const bool expands = linear_bits(L) != MOTE_SHARED_BF16 && T_max > kStreamMaxTokens;
+  return 256 + (expands ? round_up(size_t(L->N) * L->K * 2, 256) : 0);
 }
 
 extern "C" mote_status_t mote_linear(const mote_linear_t* L, const void* x, int64_t ldx, int64_t T, const void* residual, int64_t ldr,
@@ -222,7 +223,20 @@ extern "C" mote_status_t mote_linear(const mote_linear_t* L, const void* x, int6
   a.res = static_cast<const uint16_t*>(residual); a.ldr = sr; a.out = out; a.N = L->N; a.K = (int)L->K; a.act = L->act;
   a.out_f32 = out_dtype == MOTE_DTYPE_F32; a.status = static_cast<uint32_t*>(ws);
   cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-  MOTE_CUDA_OK(T <= 8 ? launch_stream<1>(a, bits, stream) : launch_stream<2>(a, bits, stream));
-  MOTE_LAUNCH_OK();
-  return MOTE_OK;
+  if (T <= kStreamMaxTokens) {
+    MOTE_CUDA_OK(T <= 8 ? launch_stream<1>(a, bits, stream) : launch_stream<2>(a, bits, stream));
+    MOTE_LAUNCH_OK();
+    return MOTE_OK;
+  }
+  if (bits == MOTE_SHARED_BF16) {
+    a.w_scale = nullptr;
+  } else {
+    void* expanded = static_cast<char*>(ws) + 256;
+    const int64_t n_chunks = L->N * L->K * bits / 64;
+    const unsigned grid = (unsigned)std::min<int64_t>((n_chunks + 255) / 256, int64_t(device_sm_count()) * 8);
+    MOTE_CUDA_OK(launch_pdl(linear_expand_kernel, dim3(grid), dim3(256), 0, stream, static_cast<const uint2*>(L->W),
+                            static_cast<uint4*>(expanded), n_chunks, bits));
+    a.W = expanded;
+  }
+  return launch_linear_umma(a, stream);
 }
