@@ -7,6 +7,8 @@
 // HBM-bound: y and the residual are read once, r' and n written once (8 bytes an element with a bf16 stream, 12 with an
 // fp32 one).  A row stays in the registers of its threads between the passes (y and r as packed vectors of 8 elements);
 // sums are fp32 in a fixed tree, so a row's result depends on its width alone.
+#include <algorithm>
+
 #include "mote_common.cuh"
 #include "mote_internal.h"
 
@@ -22,145 +24,298 @@ struct BlockNormArgs {
   int64_t gate_tokens;                   // tokens per gate row, 0: one row for all
   int d, gate_cols;                      // gate_cols: 1 or d
   int post_norm, gate_f32, gate_sigmoid;
-  float eps, scale;
+  float eps, scale, inv_d;
 };
 
-__device__ __forceinline__ void unpack8(const uint4& v, float (&f)[8]) {
-  f[0] = bf16_lo(v.x); f[1] = bf16_hi(v.x); f[2] = bf16_lo(v.y); f[3] = bf16_hi(v.y);
-  f[4] = bf16_lo(v.z); f[5] = bf16_hi(v.z); f[6] = bf16_lo(v.w); f[7] = bf16_hi(v.w);
+// Eight elements as four pairs (fp32x2 instructions work on two at a time: the kernel is as much issue- as HBM-bound).
+struct Eight { uint64_t p[4]; };
+__device__ __forceinline__ uint64_t fma_f32x2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
 }
-__device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
-  return make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
+__device__ __forceinline__ Eight unpack8(const uint4& v) {
+  Eight e;
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) e.p[j] = f32x2_bits(w[j] << 16, w[j] & 0xFFFF0000u);
+  return e;
 }
-__device__ __forceinline__ void load8_f32(const float* p, float (&f)[8]) {
+__device__ __forceinline__ uint4 pack8(const Eight& e) {
+  uint32_t w[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    float lo, hi;
+    unpack_f32x2(e.p[j], lo, hi);
+    w[j] = pack_bf16x2(lo, hi);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ Eight load8_f32(const float* p) {
   const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-  f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+  return Eight{{f32x2(a.x, a.y), f32x2(a.z, a.w), f32x2(b.x, b.y), f32x2(b.z, b.w)}};
+}
+__device__ __forceinline__ Eight operator*(const Eight& a, const Eight& b) {
+  return Eight{{mul_f32x2(a.p[0], b.p[0]), mul_f32x2(a.p[1], b.p[1]), mul_f32x2(a.p[2], b.p[2]), mul_f32x2(a.p[3], b.p[3])}};
+}
+__device__ __forceinline__ Eight operator*(const Eight& a, float s) {
+  const uint64_t b = f32x2(s, s);
+  return Eight{{mul_f32x2(a.p[0], b), mul_f32x2(a.p[1], b), mul_f32x2(a.p[2], b), mul_f32x2(a.p[3], b)}};
+}
+// sum of squares on top of a pair of sums
+__device__ __forceinline__ uint64_t add_squares(const Eight& e, uint64_t acc) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) acc = fma_f32x2(e.p[j], e.p[j], acc);
+  return acc;
 }
 __device__ __forceinline__ float sigmoid_f32(float g) { return 1.0f / (1.0f + expf(-g)); }
 
-// Sum over the row's `group` threads (whole warps); s: one slot per warp of the CTA, used once.
-__device__ __forceinline__ float group_sum(float v, int group, float* s) {
-  v = warp_sum(v);
+// Sum over a row's `group` threads (whole warps; sub: the row's number in the CTA); s: one slot per warp of the CTA.  `group` threads
+// meet at a barrier of their own.
+__device__ __forceinline__ float group_sum(uint64_t pair, int group, int sub, float* s) {
+  float lo, hi;
+  unpack_f32x2(pair, lo, hi);
+  float v = warp_sum(lo + hi);
   if (group == 32) return v;
   const int warp = threadIdx.x >> 5, per = group >> 5, first = warp / per * per;
   if ((threadIdx.x & 31) == 0) s[warp] = v;
-  __syncthreads();
-  float sum = s[first];
-  for (int i = 1; i < per; ++i) sum += s[first + i];
-  return sum;
+  asm volatile("bar.sync %0, %1;" ::"r"(sub + 1), "r"(group) : "memory");
+  v = s[first];
+  if (per == 4) {                         // the usual widths: one load
+    const float4 q = *reinterpret_cast<const float4*>(s + first);
+    return ((q.x + q.y) + q.z) + q.w;
+  }
+  for (int w = 1; w < per; ++w) v += s[first + w];
+  return v;
 }
 
-// kVec: vectors of 8 elements per thread; kResF32: type of the residual stream.  A CTA holds blockDim.x / group rows.
-template <int kVec, bool kResF32>
+template <bool kF32>
+struct Stored8 {                          // 8 elements of the residual stream as they are stored
+  uint4 v[kF32 ? 2 : 1];
+  __device__ __forceinline__ Eight get() const {
+    if (!kF32) return unpack8(v[0]);
+    const uint4 a = v[0], b = v[kF32 ? 1 : 0];
+    return Eight{{f32x2_bits(a.x, a.y), f32x2_bits(a.z, a.w), f32x2_bits(b.x, b.y), f32x2_bits(b.z, b.w)}};
+  }
+  __device__ __forceinline__ void put(const Eight& e) {        // rounds to the stored type
+    if (!kF32) { v[0] = pack8(e); return; }
+    float f[8];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) unpack_f32x2(e.p[j], f[2 * j], f[2 * j + 1]);
+    v[0] = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+    v[kF32 ? 1 : 0] = make_uint4(__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7]));
+  }
+};
+
+// A thread's weights for its columns: post_gain * act(gate) (where the gate has a value for each channel) and pre_gain.  Held in
+// registers for kVec <= 2, read where they are used for wider rows.
+template <int kVec>
+struct ColumnWeights {
+  static constexpr bool kHeld = kVec <= 2;
+  Eight mix[kHeld ? kVec : 1], pre[kHeld ? kVec : 1];
+  int64_t gate_row;                       // the gate row that `mix` holds (-1: none yet)
+};
+__device__ __forceinline__ Eight mixed_weights(const BlockNormArgs& a, int64_t gate_row, int col) {
+  Eight m;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) m.p[j] = f32x2(1.0f, 1.0f);
+  if (a.post_gain) m = load8_f32(a.post_gain + col);
+  if (a.gate_cols > 1) {
+    Eight g = a.gate_f32 ? load8_f32(static_cast<const float*>(a.gate) + gate_row * a.d + col)
+                         : unpack8(*reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.gate) + gate_row * a.d + col));
+    if (a.gate_sigmoid)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float lo, hi;
+        unpack_f32x2(g.p[j], lo, hi);
+        g.p[j] = f32x2(sigmoid_f32(lo), sigmoid_f32(hi));
+      }
+    m = m * g;
+  }
+  return m;
+}
+
+// One row.  Threads of a row that is not there (row >= T) go along as zeros.
+template <int kVec, bool kF32>
+__device__ __forceinline__ void norm_row(const BlockNormArgs& a, int64_t row, int group, int sub, int tid, const uint4 (&yv)[kVec],
+                                         Stored8<kF32> (&rv)[kVec], ColumnWeights<kVec>& cw, float* s_post, float* s_pre) {
+  constexpr bool kHeld = ColumnWeights<kVec>::kHeld;
+  const bool live = row < a.T;
+  float mul = a.scale;
+  int64_t gate_row = 0;
+  if (a.gate_cols && a.gate_tokens && live) {
+    gate_row = row;
+    if (a.gate_tokens > 1) gate_row = ((row | a.gate_tokens) >> 32) ? row / a.gate_tokens : int64_t(uint32_t(row) / uint32_t(a.gate_tokens));
+  }
+  if (a.gate_cols == 1 && live) {
+    const float g = a.gate_f32 ? static_cast<const float*>(a.gate)[gate_row]
+                               : __uint_as_float(uint32_t(static_cast<const uint16_t*>(a.gate)[gate_row]) << 16);
+    mul *= a.gate_sigmoid ? sigmoid_f32(g) : g;
+  }
+  if (a.post_norm) {
+    uint64_t ss = 0ull;
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) ss = add_squares(unpack8(yv[i]), ss);
+    mul *= rsqrtf(group_sum(ss, group, sub, s_post) * a.inv_d + a.eps);
+  }
+  const bool weighted = a.post_gain || a.gate_cols > 1;
+  const uint64_t mul2 = f32x2(mul, mul);
+  const int64_t out_at = row * a.d + tid * 8;
+  uint64_t ss = 0ull;
+#pragma unroll
+  for (int i = 0; i < kVec; ++i) {
+    const int col = (i * group + tid) * 8;
+    if (!live || col >= a.d) continue;
+    Eight p = unpack8(yv[i]);
+    if (weighted) {
+      Eight& m = cw.mix[kHeld ? i : 0];
+      if (!kHeld || gate_row != cw.gate_row) m = mixed_weights(a, gate_row, col);
+      p = p * m;
+    }
+    Eight x = rv[i].get();
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x.p[j] = fma_f32x2(p.p[j], mul2, x.p[j]);
+    rv[i].put(x);
+    if (a.res_out) {
+      uint4* o = kF32 ? reinterpret_cast<uint4*>(static_cast<float*>(a.res_out) + out_at + i * group * 8)
+                      : reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.res_out) + out_at + i * group * 8);
+#pragma unroll
+      for (int u = 0; u < (kF32 ? 2 : 1); ++u) o[u] = rv[i].v[u];
+    }
+    ss = add_squares(rv[i].get(), ss);    // the norm is that of the stored values
+  }
+  if (live) cw.gate_row = gate_row;
+  if (!a.normed_out) return;
+  const float inv = rsqrtf(group_sum(ss, group, sub, s_pre) * a.inv_d + a.eps);
+#pragma unroll
+  for (int i = 0; i < kVec; ++i) {
+    const int col = (i * group + tid) * 8;
+    if (!live || col >= a.d) continue;
+    Eight x = rv[i].get() * inv;
+    if (a.pre_gain) x = x * (kHeld ? cw.pre[kHeld ? i : 0] : load8_f32(a.pre_gain + col));
+    *reinterpret_cast<uint4*>(a.normed_out + out_at + i * group * 8) = pack8(x);
+  }
+}
+template <int kVec>
+__device__ __forceinline__ void start_weights(const BlockNormArgs& a, int group, int tid, ColumnWeights<kVec>& cw) {
+  cw.gate_row = -1;
+  if (ColumnWeights<kVec>::kHeld && a.pre_gain)
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) cw.pre[ColumnWeights<kVec>::kHeld ? i : 0] = load8_f32(a.pre_gain + min((i * group + tid) * 8, a.d - 8));
+}
+
+// A row (or several, of few threads each) per CTA.
+template <int kVec, bool kF32>
 __global__ void __launch_bounds__(512) block_norm_kernel(BlockNormArgs a, int group) {
-  __shared__ float s_post[16], s_pre[16];
+  __shared__ __align__(16) float s_post[16], s_pre[16];
   const int sub = threadIdx.x / group, tid = threadIdx.x - sub * group;
   const int64_t row = int64_t(blockIdx.x) * (blockDim.x / group) + sub;
-  const bool row_ok = row < a.T;         // a CTA's rows meet at its barriers: rows past the end go along without loads
-  const int n_vec = a.d / 8;
   pdl_wait();
   uint4 yv[kVec];
-  float rf[kVec][8];
-  const uint16_t* y = a.y + row * a.ldy;
+  Stored8<kF32> rv[kVec];
 #pragma unroll
   for (int i = 0; i < kVec; ++i) {
-    const int v = i * group + tid;
+    const int col = (i * group + tid) * 8;
+    const bool in = row < a.T && col < a.d;
     yv[i] = make_uint4(0u, 0u, 0u, 0u);
-    if (row_ok && v < n_vec) yv[i] = reinterpret_cast<const uint4*>(y)[v];
-  }
 #pragma unroll
-  for (int i = 0; i < kVec; ++i) {
-    const int v = i * group + tid;
+    for (int u = 0; u < (kF32 ? 2 : 1); ++u) rv[i].v[u] = make_uint4(0u, 0u, 0u, 0u);
+    if (in) yv[i] = *reinterpret_cast<const uint4*>(a.y + row * a.ldy + col);
+    if (in && a.res) {
+      const uint4* q = reinterpret_cast<const uint4*>(static_cast<const char*>(a.res) + (row * a.ldr + col) * (kF32 ? 4 : 2));
 #pragma unroll
-    for (int j = 0; j < 8; ++j) rf[i][j] = 0.0f;
-    if (row_ok && a.res && v < n_vec) {
-      if (kResF32) load8_f32(static_cast<const float*>(a.res) + row * a.ldr + v * 8, rf[i]);
-      else unpack8(*reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.res) + row * a.ldr + v * 8), rf[i]);
+      for (int u = 0; u < (kF32 ? 2 : 1); ++u) rv[i].v[u] = q[u];
     }
   }
-  float mul = a.scale;
-  if (a.post_norm) {
-    float ss = 0.0f;
+  ColumnWeights<kVec> cw;
+  start_weights(a, group, tid, cw);
+  norm_row<kVec, kF32>(a, row, group, sub, tid, yv, rv, cw, s_post, s_pre);
+}
+
+// Many rows: the threads of a row walk over rows.  A thread fetches its own vectors of the rows to come into shared memory
+// (cp.async; nobody else reads them, so nothing but its own copies has to be waited for), which keeps loads in flight
+// through the sums and barriers of the present row, and it holds its columns' weights all the way.
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+constexpr int kNormStages = 4;
+template <int kVec, bool kF32>
+__global__ void __launch_bounds__(256, 2) block_norm_stream_kernel(BlockNormArgs a, int group) {
+  constexpr int kUnits = 1 + (kF32 ? 2 : 1);               // 16-byte units of a thread's vector: y, and the stream's one or two
+  extern __shared__ uint4 s_ring[];                        // [stage][vector][unit][thread]
+  __shared__ __align__(16) float s_post[2][8], s_pre[2][8];
+  const int sub = threadIdx.x / group, tid = threadIdx.x - sub * group;
+  const int64_t step = int64_t(gridDim.x) * (256 / group);
+  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(s_ring) + threadIdx.x * 16;
+  auto fetch = [&](int64_t row, int stage) {
+    if (row < a.T) {
+      const uint16_t* y = a.y + row * a.ldy + tid * 8;
+      const char* res = static_cast<const char*>(a.res) + (row * a.ldr + tid * 8) * (kF32 ? 4 : 2);
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) {
+        if ((i * group + tid) * 8 >= a.d) continue;
+        const uint32_t dst = ring + ((stage * kVec + i) * kUnits) * (256 * 16);
+        cp_async16(dst, y + i * group * 8);
+        if (a.res)
+#pragma unroll
+          for (int u = 0; u < kUnits - 1; ++u) cp_async16(dst + (1 + u) * (256 * 16), res + i * group * 8 * (kF32 ? 4 : 2) + u * 16);
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  // what no copy fills (past the row's end, no residual) reads as zeros
+#pragma unroll
+  for (int i = 0; i < kNormStages * kVec * kUnits; ++i) {
+    const bool copied = ((i / kUnits % kVec) * group + tid) * 8 < a.d && (i % kUnits == 0 || a.res);
+    if (!copied) s_ring[i * 256 + threadIdx.x] = make_uint4(0u, 0u, 0u, 0u);
+  }
+  pdl_wait();
+  ColumnWeights<kVec> cw;
+  start_weights(a, group, tid, cw);
+  int64_t row = int64_t(blockIdx.x) * (256 / group) + sub;
+#pragma unroll
+  for (int s = 0; s < kNormStages - 1; ++s) fetch(row + s * step, s);
+  int stage = 0, ahead = kNormStages - 1, parity = 0;
+  for (; row < a.T; row += step) {                         // all threads of a row together
+    fetch(row + (kNormStages - 1) * step, ahead);
+    asm volatile("cp.async.wait_group %0;" ::"n"(kNormStages - 1) : "memory");
+    uint4 yv[kVec];
+    Stored8<kF32> rv[kVec];
 #pragma unroll
     for (int i = 0; i < kVec; ++i) {
-      float f[8];
-      unpack8(yv[i], f);
+      const uint4* from = s_ring + ((stage * kVec + i) * kUnits) * 256 + threadIdx.x;
+      yv[i] = from[0];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) ss = fmaf(f[j], f[j], ss);
+      for (int u = 0; u < kUnits - 1; ++u) rv[i].v[u] = from[(1 + u) * 256];
     }
-    mul = rsqrtf(group_sum(ss, group, s_post) / float(a.d) + a.eps) * a.scale;
-  }
-  int64_t grow = 0;
-  if (a.gate && row_ok) {
-    grow = a.gate_tokens ? row / a.gate_tokens : 0;
-    if (a.gate_cols == 1) {
-      float g = a.gate_f32 ? static_cast<const float*>(a.gate)[grow]
-                           : __uint_as_float(uint32_t(static_cast<const uint16_t*>(a.gate)[grow]) << 16);
-      mul *= a.gate_sigmoid ? sigmoid_f32(g) : g;
-    }
-  }
-  const bool wide_gate = a.gate && a.gate_cols != 1;
-  float ss = 0.0f;
-#pragma unroll
-  for (int i = 0; i < kVec; ++i) {
-    const int v = i * group + tid;
-    if (!row_ok || v >= n_vec) continue;
-    float p[8];
-    unpack8(yv[i], p);
-    if (a.post_norm && a.post_gain) {
-      float g[8];
-      load8_f32(a.post_gain + v * 8, g);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) p[j] *= g[j];
-    }
-    if (wide_gate) {
-      float g[8];
-      if (a.gate_f32) load8_f32(static_cast<const float*>(a.gate) + grow * a.d + v * 8, g);
-      else unpack8(*reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.gate) + grow * a.d + v * 8), g);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) p[j] *= a.gate_sigmoid ? sigmoid_f32(g[j]) : g[j];
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) rf[i][j] = fmaf(p[j], mul, rf[i][j]);
-    if (kResF32) {
-      if (a.res_out) {
-        float4* o = reinterpret_cast<float4*>(static_cast<float*>(a.res_out) + row * a.d + v * 8);
-        o[0] = make_float4(rf[i][0], rf[i][1], rf[i][2], rf[i][3]);
-        o[1] = make_float4(rf[i][4], rf[i][5], rf[i][6], rf[i][7]);
-      }
-    } else {
-      const uint4 o = pack8(rf[i]);
-      if (a.res_out) *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.res_out) + row * a.d + v * 8) = o;
-      unpack8(o, rf[i]);                 // the norm is that of the stored values
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) ss = fmaf(rf[i][j], rf[i][j], ss);
-  }
-  if (!a.normed_out) return;
-  const float inv = rsqrtf(group_sum(ss, group, s_pre) / float(a.d) + a.eps);
-#pragma unroll
-  for (int i = 0; i < kVec; ++i) {
-    const int v = i * group + tid;
-    if (!row_ok || v >= n_vec) continue;
-    float n[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) n[j] = rf[i][j] * inv;
-    if (a.pre_gain) {
-      float g[8];
-      load8_f32(a.pre_gain + v * 8, g);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) n[j] *= g[j];
-    }
-    *reinterpret_cast<uint4*>(a.normed_out + row * a.d + v * 8) = pack8(n);
+    norm_row<kVec, kF32>(a, row, group, sub, tid, yv, rv, cw, s_post[parity], s_pre[parity]);
+    ahead = stage;
+    stage = stage + 1 == kNormStages ? 0 : stage + 1;
+    parity ^= 1;
   }
 }
 
 template <int kVec>
-static cudaError_t launch_block_norm_vec(const BlockNormArgs& a, bool res_f32, int group, cudaStream_t stream) {
-  const int threads = group < 128 ? 128 : group;
-  const unsigned grid = (unsigned)((a.T + threads / group - 1) / (threads / group));
+static cudaError_t launch_block_norm(const BlockNormArgs& a, bool res_f32, int group, cudaStream_t stream) {
+  const int threads = std::max(group, 128), rows = threads / group;
+  const unsigned grid = (unsigned)((a.T + rows - 1) / rows);
   return res_f32 ? launch_pdl(block_norm_kernel<kVec, true>, dim3(grid), dim3(threads), 0, stream, a, group)
                  : launch_pdl(block_norm_kernel<kVec, false>, dim3(grid), dim3(threads), 0, stream, a, group);
+}
+template <int kVec, bool kF32>
+static cudaError_t launch_stream_as(const BlockNormArgs& a, int group, cudaStream_t stream) {
+  const int smem = kNormStages * kVec * (kF32 ? 3 : 2) * 16 * 256;
+  static PerDeviceOnce once;
+  const cudaError_t e = set_max_dynamic_smem(once, block_norm_stream_kernel<kVec, kF32>, smem);
+  if (e != cudaSuccess) return e;
+  const int64_t blocks = (a.T + 256 / group - 1) / (256 / group);
+  const int per_sm = std::min(2, 220 * 1024 / (smem + 2048));
+  return launch_pdl(block_norm_stream_kernel<kVec, kF32>, dim3((unsigned)std::min<int64_t>(blocks, device_sm_count() * per_sm)), dim3(256), smem,
+                    stream, a, group);
+}
+template <int kVec>
+static cudaError_t launch_block_norm_stream(const BlockNormArgs& a, bool res_f32, int group, cudaStream_t stream) {
+  return res_f32 ? launch_stream_as<kVec, true>(a, group, stream) : launch_stream_as<kVec, false>(a, group, stream);
 }
 
 // [a, a + na) and [b, b + nb) share a byte
@@ -209,19 +364,26 @@ extern "C" mote_status_t mote_block_norm(const mote_block_norm_t* N, const void*
   a.y = static_cast<const uint16_t*>(y); a.ldy = ldy; a.res = residual; a.ldr = ldr;
   a.gate = N->gate_cols ? gate : nullptr; a.gate_cols = N->gate_cols; a.gate_tokens = N->gate_tokens;
   a.gate_f32 = N->gate_dtype == MOTE_DTYPE_F32; a.gate_sigmoid = N->gate_sigmoid != 0;
-  a.post_norm = N->post_norm != 0; a.post_gain = N->post_gain; a.pre_gain = N->pre_gain;
+  a.post_norm = N->post_norm != 0; a.post_gain = N->post_norm ? N->post_gain : nullptr; a.pre_gain = N->pre_gain;
   a.res_out = res_out; a.normed_out = static_cast<uint16_t*>(normed_out);
-  a.T = T; a.d = (int)d; a.eps = N->eps; a.scale = N->scale;
+  a.T = T; a.d = (int)d; a.eps = N->eps; a.scale = N->scale; a.inv_d = 1.0f / float(d);
   const int n_vec = (int)d / 8;
-  // Threads of a row: with rows to fill the GPU, up to four vectors a thread; with few, one.
-  int vec = T > 1024 ? 4 : T > 256 ? 2 : 1;
-  while (vec * 512 < n_vec) vec *= 2;
-  int group = 32;
-  while (group * vec < n_vec) group *= 2;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  MOTE_CUDA_OK(vec == 8 ? launch_block_norm_vec<8>(a, f32, group, s)
-               : vec == 4 ? launch_block_norm_vec<4>(a, f32, group, s)
-               : vec == 2 ? launch_block_norm_vec<2>(a, f32, group, s) : launch_block_norm_vec<1>(a, f32, group, s));
+  cudaError_t e;
+  // Threads of a row, by its width alone, so that a row's sums do not depend on T: two vectors a thread (one in rows of up to 256
+  // elements), more where that takes over 256 threads, and up to 512 threads for rows of more than 8192 elements.
+  const int most = n_vec <= 1024 ? 256 : 512;
+  int vec = n_vec <= 32 ? 1 : 2, group = 32;
+  while (vec * most < n_vec) vec *= 2;
+  while (group * vec < n_vec) group *= 2;
+  if (n_vec <= 1024 && T >= int64_t(device_sm_count()) * 8)            // rows enough to walk over
+    e = vec == 4   ? launch_block_norm_stream<4>(a, f32, group, s)
+        : vec == 2 ? launch_block_norm_stream<2>(a, f32, group, s) : launch_block_norm_stream<1>(a, f32, group, s);
+  else
+    e = vec == 8   ? launch_block_norm<8>(a, f32, group, s)
+        : vec == 4 ? launch_block_norm<4>(a, f32, group, s)
+        : vec == 2 ? launch_block_norm<2>(a, f32, group, s) : launch_block_norm<1>(a, f32, group, s);
+  if (e != cudaSuccess) return MOTE_ERR_CUDA;
   MOTE_LAUNCH_OK();
   return MOTE_OK;
 }

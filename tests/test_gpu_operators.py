@@ -235,6 +235,19 @@ def test_block_norm_in_place_strided_and_partial_outputs(mote):
     assert empty[0].shape == (0, d) and empty[1].shape == (0, d)
 
 
+@pytest.mark.parametrize("d", [64, 896, 2048, 4096, 8192, 8200])
+def test_block_norm_rows_do_not_depend_on_the_batch(mote, d):
+    y, res, gate = _randn(26, 2500, d).bfloat16(), _randn(27, 2500, d).bfloat16(), _randn(28, 2500, d).bfloat16()
+    norm = mote.MoteBlockNorm(d, post_norm=True, post_gain=1.0 + 0.1 * _randn(29, d), gate_sigmoid=True)
+    whole = mote.mote_block_norm(norm, y, res, gate=gate)
+    for a, b in ((0, 1), (3, 300), (1100, 2500)):
+        part = mote.mote_block_norm(norm, y[a:b], res[a:b], gate=gate[a:b])
+        assert torch.equal(part[0], whole[0][a:b]) and torch.equal(part[1], whole[1][a:b])
+    # in the place of its inputs, with rows on the way
+    r, n = mote.mote_block_norm(norm, y, res, gate=gate, res_out=res, normed_out=y)
+    assert torch.equal(r, whole[0]) and torch.equal(n, whole[1])
+
+
 # ------------------------------------------------------------------------------------------------ projections
 def make_linear(mote, N, K, bits, bias, act, seed):
     W = (_randn(seed, N, K) * 0.05).bfloat16()
