@@ -1,5 +1,6 @@
-"""ctypes binding of libmote.so.  Argument marshalling only: every step of the layer runs in the
-library's kernels.  torch is used for device memory and streams."""
+"""Binding of libmote.so: ctypes, and for the operators that run on a token or a few the extension module _calls (csrc/torch_calls.cpp),
+whose calls take less time.  Argument marshalling only: every step runs in the library's kernels.  torch is used for device
+memory and streams."""
 from __future__ import annotations
 
 import ctypes as C
@@ -13,6 +14,11 @@ if not os.path.exists(_LIB_PATH):
     raise ImportError(f"{_LIB_PATH} is missing: build it with `python -m paper_2506_14435_b200.build`; "
                       "there is no fallback path")
 lib = C.CDLL(_LIB_PATH)
+try:
+    from . import _calls
+except ImportError as e:
+    raise ImportError("paper_2506_14435_b200/_calls.so is missing or was built for another torch: build it with "
+                      "`python -m paper_2506_14435_b200.build`") from e
 
 PATH_AUTO, PATH_SIMT, PATH_TENSOR, PATH_STREAM = 0, 1, 2, 3
 DTYPE_F32, DTYPE_BF16 = 0, 1
@@ -246,13 +252,6 @@ def _here(dev: int):
         raise ValueError("expected tensors on the current CUDA device")
 
 
-def _rows(t: torch.Tensor, name: str, dtype, shape, dev: int) -> int:
-    """Row stride of a [rows, cols] CUDA matrix with unit inner stride."""
-    if t.dtype is not dtype or t.get_device() != dev or tuple(t.shape) != shape or (t.stride(1) != 1 and shape[1] > 1):
-        raise ValueError(f"{name}: expected {dtype} {list(shape)} with unit inner stride on cuda:{dev}")
-    return t.stride(0) if shape[0] > 1 else shape[1]
-
-
 def _vector(t, name: str, n: int, dev):
     """An optional [n] float32 weight, and its address."""
     if t is None:
@@ -286,21 +285,15 @@ class MoteRouter:
         self.tensors = dict(Wr=Wr, logit_bias=lb, select_bias=sb, packed=packed)
         self.struct = mote_router_t(self.d, self.E, k, {"softmax": 0, "sigmoid": 1}[scoring], n_groups, topk_groups, int(renorm), scale,
                                     Wr.data_ptr(), dt, lb_ptr, sb_ptr, packed.data_ptr())
-        self._ref = C.byref(self.struct)
+        self._address = C.addressof(self.struct)
 
 
 def mote_route_scored(router: MoteRouter, x: torch.Tensor, want_logits: bool = False):
     """x[T, d] bf16 (rows may be strided) -> (topk_idx int32[T, k], topk_w f32[T, k], logits f32[T, E] or None)."""
-    T = x.shape[0]
-    dev = router.device
-    _here(dev)
-    ldx = _rows(x, "x", torch.bfloat16, (T, router.d), dev)
-    idx = torch.empty((T, router.k), dtype=torch.int32, device=x.device)
-    w = torch.empty((T, router.k), dtype=torch.float32, device=x.device)
-    logits = torch.empty((T, router.E), dtype=torch.float32, device=x.device) if want_logits else None
-    _check(lib.mote_route_scored(router._ref, x.data_ptr(), ldx, T, idx.data_ptr(), w.data_ptr(),
-                                 logits.data_ptr() if want_logits else None, _stream()), "mote_route_scored")
-    return idx, w, logits
+    r = _calls.route_scored(router._address, router.device, x, want_logits)
+    if type(r) is int:
+        raise MoteError(r, "mote_route_scored")
+    return r
 
 
 class MoteBlockNorm:
@@ -308,61 +301,24 @@ class MoteBlockNorm:
     a row of the gate (1: a row each, 0: one row for all)."""
 
     def __init__(self, d, eps=1e-6, post_norm=False, post_gain=None, pre_gain=None, scale=1.0, gate_sigmoid=False, gate_tokens=1):
-        self.d, self.gate_tokens = d, gate_tokens
         pg, pg_ptr = _vector(post_gain, "post_gain", d, None)
         ng, ng_ptr = _vector(pre_gain, "pre_gain", d, pg.get_device() if pg is not None else None)
         self.device = pg.get_device() if pg is not None else ng.get_device() if ng is not None else None
+        self._device = -1 if self.device is None else self.device
         self.tensors = dict(post_gain=pg, pre_gain=ng)
-        # residual type, columns and type of the gate: (1, 0, 0) and the like, filled in by the call
-        self._args = (d, eps, scale, int(post_norm), pg_ptr, ng_ptr), (int(gate_sigmoid), gate_tokens)
-        self._structs = {}
-
-    def struct(self, res_dtype: int, gate_cols: int, gate_dtype: int):
-        key = (res_dtype, gate_cols, gate_dtype)
-        ref = self._structs.get(key)
-        if ref is None:
-            ref = self._structs[key] = C.byref(mote_block_norm_t(*self._args[0], *key, *self._args[1]))
-        return ref
+        # the types of the residual and the gate, and the gate's columns, are the call's
+        self.struct = mote_block_norm_t(d, eps, scale, int(post_norm), pg_ptr, ng_ptr, DTYPE_BF16, 0, DTYPE_F32, int(gate_sigmoid), gate_tokens)
+        self._address = C.addressof(self.struct)
 
 
 def mote_block_norm(norm: MoteBlockNorm, y: torch.Tensor, residual=None, gate=None, res_out=None, normed_out=None,
                     want_residual: bool = True, want_normed: bool = True):
     """y[T, d] bf16 -> (res_out [T, d] of the residual's type, normed_out [T, d] bf16); either is None where not wanted.  gate:
     [rows, 1] or [rows, d], bf16 or fp32, with rows = ceil(T / gate_tokens).  res_out may be residual, normed_out may be y."""
-    d = norm.d
-    T = y.shape[0]
-    dev = y.get_device()
-    _here(dev)
-    if norm.device is not None and norm.device != dev:
-        raise ValueError("the gains are on another device")
-    ldy = _rows(y, "y", torch.bfloat16, (T, d), dev)
-    res_dtype = torch.bfloat16
-    if residual is not None:
-        res_dtype = residual.dtype
-    elif res_out is not None:
-        res_dtype = res_out.dtype
-    if res_dtype not in _DTYPES:
-        raise ValueError("residual: expected float32 or bfloat16")
-    ldr = _rows(residual, "residual", res_dtype, (T, d), dev) if residual is not None else d
-    cols, gate_dt = 0, 0
-    if gate is not None:
-        rows = min(T, 1) if norm.gate_tokens == 0 else -(-T // norm.gate_tokens)
-        cols = gate.shape[1] if gate.dim() == 2 else -1
-        if cols not in (1, d) or gate.shape[0] != rows or gate.dtype not in _DTYPES or not gate.is_contiguous() or gate.get_device() != dev:
-            raise ValueError(f"gate: expected contiguous float32 or bfloat16 [{rows}, 1] or [{rows}, {d}]")
-        gate_dt = _DTYPES[gate.dtype]
-    for name, o, dt in (("res_out", res_out, res_dtype), ("normed_out", normed_out, torch.bfloat16)):
-        if o is not None and (_rows(o, name, dt, (T, d), dev) != d):
-            raise ValueError(f"{name}: expected contiguous rows")
-    if res_out is None and want_residual:
-        res_out = torch.empty((T, d), dtype=res_dtype, device=y.device)
-    if normed_out is None and want_normed:
-        normed_out = torch.empty((T, d), dtype=torch.bfloat16, device=y.device)
-    _check(lib.mote_block_norm(norm.struct(_DTYPES[res_dtype], cols, gate_dt), y.data_ptr(), ldy,
-                               None if residual is None else residual.data_ptr(), ldr, None if gate is None else gate.data_ptr(), T,
-                               None if res_out is None else res_out.data_ptr(), None if normed_out is None else normed_out.data_ptr(),
-                               _stream()), "mote_block_norm")
-    return res_out, normed_out
+    r = _calls.block_norm(norm._address, norm._device, y, residual, gate, res_out, normed_out, want_residual, want_normed)
+    if type(r) is int:
+        raise MoteError(r, "mote_block_norm")
+    return r
 
 
 ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}
@@ -386,9 +342,10 @@ class MoteLinear:
         b, b_ptr = _vector(bias, "bias", self.N, self.device)
         self.tensors = dict(W=W, scale=sc, bias=b)
         self.struct = mote_linear_t(self.N, self.K, W.data_ptr(), bits, sc_ptr, b_ptr, ACTS[act])
-        self._ref = C.byref(self.struct)
+        self._address = C.addressof(self.struct)
         self._ws = None
         self._ws_T = -1                      # the workspace serves up to this many tokens
+        self._ws_address = self._ws_bytes = 0
 
     @classmethod
     def quantized(cls, W, bits, bias=None, act="none"):
@@ -398,11 +355,12 @@ class MoteLinear:
 
     def workspace(self, T: int) -> torch.Tensor:
         if T > self._ws_T:
-            need = lib.mote_linear_workspace_bytes(self._ref, T)
+            need = lib.mote_linear_workspace_bytes(C.byref(self.struct), T)
             if need == 0:
                 raise MoteError(2, "mote_linear_workspace_bytes")
-            if self._ws is None or self._ws.numel() < need:
+            if need > self._ws_bytes:
                 self._ws = torch.empty(need, dtype=torch.uint8, device=self.tensors["W"].device)
+                self._ws_address, self._ws_bytes = self._ws.data_ptr(), need
             self._ws_T = T
         return self._ws
 
@@ -410,20 +368,12 @@ class MoteLinear:
 def mote_linear(linear: MoteLinear, x: torch.Tensor, residual=None, out=None, out_dtype=torch.bfloat16):
     """x[T, K] bf16 (rows may be strided) -> act(x W^T + bias) + residual, [T, N] of out_dtype (or out's type); out may be
     residual.  Uses the layer's own workspace: calls of one MoteLinear that can run at the same time need one object each."""
-    T, dev = x.shape[0], linear.device
-    _here(dev)
-    ldx = _rows(x, "x", torch.bfloat16, (T, linear.K), dev)
-    ldr = _rows(residual, "residual", torch.bfloat16, (T, linear.N), dev) if residual is not None else linear.N
-    if out is None:
-        out = torch.empty((T, linear.N), dtype=out_dtype, device=x.device)
-    elif out.dtype not in _DTYPES or _rows(out, "out", out.dtype, (T, linear.N), dev) != linear.N:
-        raise ValueError("out: expected contiguous float32 or bfloat16 rows")
-    if out.dtype not in _DTYPES:
-        raise ValueError("out_dtype: expected float32 or bfloat16")
-    ws = linear.workspace(T)
-    _check(lib.mote_linear(linear._ref, x.data_ptr(), ldx, T, None if residual is None else residual.data_ptr(), ldr, out.data_ptr(),
-                           _DTYPES[out.dtype], ws.data_ptr(), ws.numel(), _stream()), "mote_linear")
-    return out
+    if len(x) > linear._ws_T:
+        linear.workspace(len(x))
+    r = _calls.linear(linear._address, linear.device, x, residual, out, out_dtype, linear._ws_address, linear._ws_bytes)
+    if type(r) is int:
+        raise MoteError(r, "mote_linear")
+    return r
 
 
 class MoteLayer:
@@ -560,7 +510,7 @@ def mote_moe_forward_scored(layer: MoteLayer, router: MoteRouter, x: torch.Tenso
         for n, t in taps.items():
             setattr(tp, n, t.data_ptr())
         tp = C.byref(tp)
-    _check(lib.mote_moe_forward_scored(C.byref(s), router._ref, _ptr(x), _ptr(residual), T, _ptr(out), tp, _ptr(ws), ws.numel(),
+    _check(lib.mote_moe_forward_scored(C.byref(s), C.byref(router.struct), _ptr(x), _ptr(residual), T, _ptr(out), tp, _ptr(ws), ws.numel(),
                                        _stream()), "mote_moe_forward_scored")
     return out
 

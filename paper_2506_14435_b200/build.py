@@ -1,9 +1,11 @@
-"""Builds libmote.so (sm_100a) in-tree with nvcc.  Usage: python -m paper_2506_14435_b200.build"""
+"""Builds libmote.so (sm_100a) in-tree with nvcc, and _calls.so, the extension module of the binding, with g++ against torch.
+Usage: python -m paper_2506_14435_b200.build"""
 from __future__ import annotations
 
 import os
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -11,6 +13,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libmote.so")
+CALLS = os.path.join(PKG, "_calls.so")
 
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 # never -use_fast_math: the pinned fp32 sequences need IEEE division and no flush-to-zero
@@ -44,9 +47,29 @@ def _compile(src: str, verbose: bool) -> str:
     return obj
 
 
+def _compile_calls() -> str:
+    """torch_calls.cpp -> an object file for the installed torch (its C++ interface is not stable between versions)."""
+    import torch
+    src = os.path.join(CSRC, "torch_calls.cpp")
+    obj = os.path.join(OBJ, f"torch_calls-{torch.__version__}-{sys.implementation.cache_tag}.o")
+    if os.path.exists(obj) and os.path.getmtime(obj) > max(os.path.getmtime(src), _newest_header()):
+        return obj
+    inc = os.path.join(os.path.dirname(torch.__file__), "include")
+    cuda = os.path.join(os.path.dirname(os.path.dirname(NVCC)), "include")
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           "-I" + os.path.join(ROOT, "include"), "-isystem", inc, "-isystem", os.path.join(inc, "torch", "csrc", "api", "include"),
+           "-isystem", sysconfig.get_paths()["include"], "-isystem", cuda, "-c", src, "-o", obj]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode:
+        sys.stderr.write(r.stdout + r.stderr)
+        raise RuntimeError("g++ failed on torch_calls.cpp")
+    return obj
+
+
 def build(verbose: bool = False) -> str:
     os.makedirs(OBJ, exist_ok=True)
     with ThreadPoolExecutor(max_workers=8) as ex:
+        calls = ex.submit(_compile_calls)
         objs = list(ex.map(lambda s: _compile(s, verbose), _sources()))
     if not os.path.exists(LIB) or any(os.path.getmtime(o) > os.path.getmtime(LIB) for o in objs):
         cmd = [NVCC, "-shared", "-o", LIB, *objs, "-cudart", "static"]
@@ -54,6 +77,16 @@ def build(verbose: bool = False) -> str:
         if r.returncode:
             sys.stderr.write(r.stdout + r.stderr)
             raise RuntimeError("link failed")
+    calls = calls.result()
+    if not os.path.exists(CALLS) or os.path.getmtime(CALLS) < os.path.getmtime(calls):
+        import torch
+        libs = os.path.join(os.path.dirname(torch.__file__), "lib")
+        cmd = ["g++", "-shared", "-o", CALLS, calls, "-L" + PKG, "-l:libmote.so", "-Wl,-rpath,$ORIGIN", "-L" + libs,
+               "-ltorch_python", "-ltorch_cuda", "-ltorch_cpu", "-lc10_cuda", "-lc10"]
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        if r.returncode:
+            sys.stderr.write(r.stdout + r.stderr)
+            raise RuntimeError("link of _calls.so failed")
     return LIB
 
 

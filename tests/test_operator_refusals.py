@@ -172,6 +172,10 @@ def test_python_calls_refuse_tensors_that_are_not_on_a_gpu(b):
         b.MoteLinear(torch.zeros(4, 64, dtype=torch.bfloat16))
     with pytest.raises(ValueError):
         b.MoteBlockNorm(64, pre_gain=torch.zeros(64))
+    with pytest.raises(ValueError):
+        b.mote_block_norm(b.MoteBlockNorm(64), torch.zeros(3, 64, dtype=torch.bfloat16))
+    with pytest.raises(ValueError):
+        b.mote_block_norm(b.MoteBlockNorm(64), [1.0])
 
 
 # ------------------------------------------------------------------------------------------------ the statements themselves
