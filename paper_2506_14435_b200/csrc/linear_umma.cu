@@ -5,7 +5,7 @@
 // advances 64 elements, 128 bytes of either operand, per pipeline stage, four K = 16 MMAs each.  What lies beyond the tensors is zero
 // (TMA fill) and is not stored.
 //
-// Warp roles: 0 TMA producer, 1 MMA issuer, 2 TMEM owner, 4 to 11 epilogue (two per TMEM lane quarter, which share the tile's columns).
+// Warp roles: 0 TMA producer, 1 MMA issuer, 2 TMEM owner, 4 to 19 epilogue (four per TMEM lane quarter, which share the tile's columns).
 // Three forms:
 //   pairs of CTAs (CG = 2)   cta_group::2 MMAs read half of the weight rows from either CTA: a tile of 256 x 256 fetches 32 KB a stage and
 //                            SM, two thirds of what two tiles of 128 x 256 do
@@ -26,12 +26,13 @@ namespace mote {
 
 using namespace ptx;
 
-constexpr int kLinThreads = 384;
-constexpr int kLinEpiFirst = 4, kLinEpiWarps = 8;
+constexpr int kLinEpiFirst = 4, kLinEpiWarps = 16, kLinParts = kLinEpiWarps / 4;
+constexpr int kLinThreads = (kLinEpiFirst + kLinEpiWarps) * 32;
 constexpr int kLinStageA = 128 * 128;            // 128 rows x 128 bytes
 constexpr int kLinMaxStages = 8;
-constexpr int kLinPipeBytes = 192 * 1024;
-constexpr int kLinPitch = 17;                    // floats per row of an epilogue warp's staging block
+constexpr int kLinPipeBytes = 192 * 1024;         // the stages' share of shared memory; less where rows of out have no alignment:
+constexpr int kLinPipeBytesOdd = 148 * 1024;      // the epilogue then puts its rows together in shared memory
+constexpr int kLinPitch = 33;                     // words per row of an epilogue warp's block for that: 64 bf16 or 32 fp32 values
 constexpr int kLinStaging = kLinEpiWarps * 32 * kLinPitch * 4;
 
 struct LinearTiles {
@@ -47,96 +48,146 @@ struct __align__(8) LinearBarriers {
   uint32_t tmem_base;
   int abort_flag;
 };
-constexpr int kLinSmem = 1024 + kLinPipeBytes + kLinStaging + (int)sizeof(LinearBarriers);
+constexpr int kLinColumns = kLinEpiWarps * 2 * 64 * 4;      // scale and bias of an epilogue warp's columns
+constexpr int kLinPastPipe = std::max(kLinPipeBytes, kLinPipeBytesOdd + kLinStaging);
+constexpr int kLinSmem = 1024 + kLinPastPipe + kLinColumns + (int)sizeof(LinearBarriers);
+static_assert(kLinSmem <= 227 * 1024, "shared memory of a CTA");
 
 __device__ __forceinline__ void linear_item(const LinearTiles& t, int item, int& mt, int& nt) {
   if (t.rows_fast) { mt = item % t.n_mt; nt = item / t.n_mt; }
   else { nt = item % t.n_nt; mt = item / t.n_nt; }
 }
 
-// Finishes 16 neighbouring columns of a warp's 32 rows (lane = row): scale, bias, activation, residual, one rounding.
-__device__ __forceinline__ void finish_columns(const LinearArgs& a, const LinearTiles& t, float (&z)[16], int64_t row0, int64_t col, float* stg,
-                                               int lane) {
-  if (a.w_scale || a.bias) {
-    if (col + 16 <= a.N) {                       // col is a multiple of 16, so these vectors are aligned
+// Scale and bias of an epilogue warp's `n` (up to 64) columns from col0 on, into its own block; asked for before the accumulator is
+// complete.
+__device__ __forceinline__ void load_columns(const LinearArgs& a, int64_t col0, int n, float* cols, int lane) {
+  __syncwarp();
 #pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        if (a.w_scale) {
-          const float4 s = __ldg(reinterpret_cast<const float4*>(a.w_scale + col) + v);
-          z[4 * v] *= s.x; z[4 * v + 1] *= s.y; z[4 * v + 2] *= s.z; z[4 * v + 3] *= s.w;
-        }
-        if (a.bias) {
-          const float4 b = __ldg(reinterpret_cast<const float4*>(a.bias + col) + v);
-          z[4 * v] += b.x; z[4 * v + 1] += b.y; z[4 * v + 2] += b.z; z[4 * v + 3] += b.w;
-        }
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < 16; ++j)
-        if (col + j < a.N) {
-          if (a.w_scale) z[j] *= __ldg(a.w_scale + col + j);
-          if (a.bias) z[j] += __ldg(a.bias + col + j);
-        }
+  for (int i = lane; i < 64; i += 32) {
+    if (a.w_scale && i < n) cols[i] = __ldg(a.w_scale + col0 + i);
+    if (a.bias && i < n) cols[64 + i] = __ldg(a.bias + col0 + i);
+  }
+  __syncwarp();
+}
+
+// The residual of 16 neighbouring columns of a row, where rows lie on 16-byte boundaries.
+__device__ __forceinline__ void load_residual(const LinearArgs& a, const LinearTiles& t, int64_t row, int64_t col, uint4 (&r)[2]) {
+  if (!a.res || !t.vec8 || row >= a.T) return;
+  const uint4* rp = reinterpret_cast<const uint4*>(a.res + row * a.ldr + col);
+  if (col < a.N) r[0] = rp[0];
+  if (col + 8 < a.N) r[1] = rp[1];
+}
+
+// Writes the `n` columns from col on that a warp has put together in its block, 32 rows from row0 on: neighbouring lanes write
+// neighbouring elements, on any boundary.
+__device__ __forceinline__ void write_rows(const LinearArgs& a, int64_t row0, int64_t col, int n, const uint32_t* stg, int lane) {
+  __syncwarp();
+  const int rows = (int)min(int64_t(32), a.T - row0);
+  if (a.out_f32) {
+    float* o = static_cast<float*>(a.out) + row0 * a.N + col + lane;
+    const bool in = lane < n;
+    const uint32_t* from = stg + lane;
+#pragma unroll 8
+    for (int r = 0; r < rows; ++r, o += a.N)
+      if (in) *o = __uint_as_float(from[r * kLinPitch]);
+  } else {
+    uint16_t* o = static_cast<uint16_t*>(a.out) + row0 * a.N + col + lane;
+    const uint16_t* from = reinterpret_cast<const uint16_t*>(stg) + lane;
+    const bool in0 = lane < n, in1 = lane + 32 < n;
+#pragma unroll 8
+    for (int r = 0; r < rows; ++r, o += a.N) {
+      if (in0) o[0] = from[r * 2 * kLinPitch];
+      if (in1) o[32] = from[r * 2 * kLinPitch + 32];
     }
   }
-  if (a.act != MOTE_ACT_NONE) {
+  __syncwarp();
+}
+
+// Finishes 16 neighbouring columns of a warp's 32 rows (lane = row): scale, bias, activation, residual, one rounding.  Stored at once
+// where rows lie on 16-byte boundaries, else put at column `at` of the warp's block.
+__device__ __forceinline__ void finish_columns(const LinearArgs& a, const LinearTiles& t, uint64_t (&z)[8], const uint4 (&res)[2], int64_t row0,
+                                               int64_t col, const float* cols, uint32_t* stg, int at, int lane) {
+  if (a.w_scale) {
 #pragma unroll
-    for (int j = 0; j < 16; ++j) z[j] = apply_act(z[j], a.act);
+    for (int v = 0; v < 4; ++v) {
+      const ulonglong2 s = reinterpret_cast<const ulonglong2*>(cols)[v];
+      z[2 * v] = mul_f32x2(z[2 * v], s.x);
+      z[2 * v + 1] = mul_f32x2(z[2 * v + 1], s.y);
+    }
   }
+  if (a.bias) {
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      const ulonglong2 b = reinterpret_cast<const ulonglong2*>(cols + 64)[v];
+      z[2 * v] = add_f32x2(z[2 * v], b.x);
+      z[2 * v + 1] = add_f32x2(z[2 * v + 1], b.y);
+    }
+  }
+  apply_act16(z, a.act);
   const int64_t row = row0 + lane;
-  if (t.vec8) {                                  // N is a multiple of 8: each half of the 16 columns is inside or outside as a whole
-    if (row >= a.T || col >= a.N) return;
-    const bool both = col + 16 <= a.N;
-    if (a.res) {
-      const uint4* rp = reinterpret_cast<const uint4*>(a.res + row * a.ldr + col);
+  if (a.res) {
+    if (t.vec8) {                                // a half that lies outside is not stored
+      const uint32_t w[8] = {res[0].x, res[0].y, res[0].z, res[0].w, res[1].x, res[1].y, res[1].z, res[1].w};
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-        if (h == 0 || both) {
-          const uint4 r = rp[h];
-          const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+      for (int j = 0; j < 8; ++j) z[j] = add_f32x2(z[j], f32x2_bits(w[j] << 16, w[j] & 0xFFFF0000u));
+    } else if (row < a.T) {
+      const uint16_t* rp = a.res + row * a.ldr + col;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) { z[8 * h + 2 * j] += bf16_lo(w[j]); z[8 * h + 2 * j + 1] += bf16_hi(w[j]); }
-        }
-    }
-    if (a.out_f32) {
-      float* o = static_cast<float*>(a.out) + row * a.N + col;
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-        if (h == 0 || both) {
-          if (t.wide) {
-            st_global_v8(o + 8 * h, __float_as_uint(z[8 * h]), __float_as_uint(z[8 * h + 1]), __float_as_uint(z[8 * h + 2]), __float_as_uint(z[8 * h + 3]),
-                         __float_as_uint(z[8 * h + 4]), __float_as_uint(z[8 * h + 5]), __float_as_uint(z[8 * h + 6]), __float_as_uint(z[8 * h + 7]));
-          } else {
-            reinterpret_cast<float4*>(o + 8 * h)[0] = make_float4(z[8 * h], z[8 * h + 1], z[8 * h + 2], z[8 * h + 3]);
-            reinterpret_cast<float4*>(o + 8 * h)[1] = make_float4(z[8 * h + 4], z[8 * h + 5], z[8 * h + 6], z[8 * h + 7]);
-          }
-        }
-    } else {
-      uint16_t* o = static_cast<uint16_t*>(a.out) + row * a.N + col;
-      uint32_t p[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) p[j] = pack_bf16x2(z[2 * j], z[2 * j + 1]);
-      if (t.wide && both) st_global_v8(o, p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7]);
-      else {
-        reinterpret_cast<uint4*>(o)[0] = make_uint4(p[0], p[1], p[2], p[3]);
-        if (both) reinterpret_cast<uint4*>(o)[1] = make_uint4(p[4], p[5], p[6], p[7]);
+      for (int j = 0; j < 8; ++j) {
+        const uint32_t lo = col + 2 * j < a.N ? rp[2 * j] : 0u, hi = col + 2 * j + 1 < a.N ? rp[2 * j + 1] : 0u;
+        z[j] = add_f32x2(z[j], f32x2_bits(lo << 16, hi << 16));
       }
+    }
+  }
+  uint32_t w[16];                                // the values as stored: 16 words, or 8 of two bf16 each
+  if (a.out_f32) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      float lo, hi;
+      unpack_f32x2(z[j], lo, hi);
+      w[2 * j] = __float_as_uint(lo);
+      w[2 * j + 1] = __float_as_uint(hi);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      float lo, hi;
+      unpack_f32x2(z[j], lo, hi);
+      w[j] = pack_bf16x2(lo, hi);
+    }
+  }
+  if (!t.vec8) {
+    if (a.out_f32) {
+#pragma unroll
+      for (int j = 0; j < 16; ++j) stg[lane * kLinPitch + at + j] = w[j];
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) stg[lane * kLinPitch + at / 2 + j] = w[j];
     }
     return;
   }
-  // rows on any boundary: through shared memory, so that 16 lanes write 16 neighbouring elements of a row
-  __syncwarp();
+  // N is a multiple of 8: each half of the 16 columns is inside or outside as a whole
+  if (row >= a.T) return;
+  const bool both_in = col + 16 <= a.N;
+  if (a.out_f32) {
+    float* o = static_cast<float*>(a.out) + row * a.N + col;
 #pragma unroll
-  for (int j = 0; j < 16; ++j) stg[lane * kLinPitch + j] = z[j];
-  __syncwarp();
-  const int64_t c = col + (lane & 15);
-#pragma unroll 4
-  for (int r = lane >> 4; r < 32; r += 2) {
-    if (row0 + r >= a.T || c >= a.N) continue;
-    float v = stg[r * kLinPitch + (lane & 15)];
-    if (a.res) v += __uint_as_float(uint32_t(a.res[(row0 + r) * a.ldr + c]) << 16);
-    if (a.out_f32) static_cast<float*>(a.out)[(row0 + r) * a.N + c] = v;
-    else static_cast<uint16_t*>(a.out)[(row0 + r) * a.N + c] = (uint16_t)(pack_bf16x2(v, 0.0f) & 0xFFFFu);
+    for (int h = 0; h < 2; ++h)
+      if (h == 0 || both_in) {
+        const uint32_t* v = w + 8 * h;
+        if (t.wide) st_global_v8(o + 8 * h, v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]);
+        else {
+          reinterpret_cast<uint4*>(o + 8 * h)[0] = make_uint4(v[0], v[1], v[2], v[3]);
+          reinterpret_cast<uint4*>(o + 8 * h)[1] = make_uint4(v[4], v[5], v[6], v[7]);
+        }
+      }
+  } else {
+    uint16_t* o = static_cast<uint16_t*>(a.out) + row * a.N + col;
+    if (t.wide) st_global_v8(o, w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7]);
+    else {
+      reinterpret_cast<uint4*>(o)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+      if (both_in) reinterpret_cast<uint4*>(o)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    }
   }
 }
 
@@ -156,8 +207,9 @@ linear_umma_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
   uint8_t* smem_gen = smem_raw + (smem_base - smem_u32(smem_raw));
   const uint32_t stage_b = uint32_t(t.bn / CG) * 128;
   const uint32_t stage_bytes = kLinStageA + stage_b;
-  float* staging = reinterpret_cast<float*>(smem_gen + kLinPipeBytes);
-  LinearBarriers* bars = reinterpret_cast<LinearBarriers*>(smem_gen + kLinPipeBytes + kLinStaging);
+  uint32_t* staging = reinterpret_cast<uint32_t*>(smem_gen + kLinPipeBytesOdd);      // used where t.vec8 is not set
+  float* column_data = reinterpret_cast<float*>(smem_gen + kLinPastPipe);
+  LinearBarriers* bars = reinterpret_cast<LinearBarriers*>(smem_gen + kLinPastPipe + kLinColumns);
   volatile int* abort_flag = &bars->abort_flag;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const uint32_t rank = (CG == 2 || kSplit) ? cluster_ctarank() : 0;
@@ -251,27 +303,42 @@ linear_umma_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
     }
   } else if (warp >= kLinEpiFirst && !kSplit) {
     const int q = warp & 3, part = (warp - kLinEpiFirst) >> 2;
-    float* stg = staging + (warp - kLinEpiFirst) * 32 * kLinPitch;
+    uint32_t* stg = staging + (warp - kLinEpiFirst) * 32 * kLinPitch;
+    float* cols = column_data + (warp - kLinEpiFirst) * 128;
+    const int share = (t.bn / kLinParts + 15) & ~15;            // columns of one of the warps of a lane quarter, up to 64
+    const int room = a.out_f32 ? 32 : 64;                       // columns that a warp's block holds
     int local = 0;
     for (int item = worker; item < n_items; item += workers, ++local) {
       int mt, nt;
       linear_item(t, item, mt, nt);
       const int buf = local & 1;
+      const int64_t row0 = int64_t(mt * CG + (CG == 2 ? (int)rank : 0)) * 128 + q * 32, col0 = int64_t(nt) * t.bn + part * share;
+      const uint32_t t_row = tmem_base + (uint32_t(q * 32) << 16) + buf * 256 + part * share;
+      // columns of this warp that are there (a warp beyond the last row has none)
+      const int n = row0 < a.T ? (int)max(int64_t(0), min(int64_t(min(share, t.bn - part * share)), a.N - col0)) : 0;
+      if (n > 0) load_columns(a, col0, n, cols, lane);
+      uint4 res[2];
+      if (n > 0) load_residual(a, t, row0 + lane, col0, res);
       if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->tmem_full[buf]), (local >> 1) & 1, abort_flag))) break;
       tc_fence_after();
-      const uint32_t t_row = tmem_base + (uint32_t(q * 32) << 16) + buf * 256;
-      const int64_t row0 = int64_t(mt * CG + (CG == 2 ? (int)rank : 0)) * 128 + q * 32;
+      int put = 0;
 #pragma unroll 1
-      for (int c = part * 16; c < t.bn; c += 32) {
-        const int64_t col = int64_t(nt) * t.bn + c;
-        if (row0 >= a.T || col >= a.N) continue;   // whole warp
+      for (int c = 0; c < n; c += 16) {
         uint32_t r[16];
         tmem_ld_32x32b_x16(t_row + c, r);
+        if (c > 0) load_residual(a, t, row0 + lane, col0 + c, res);
         tmem_wait_ld();
-        float z[16];
+        uint64_t z[8];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) z[j] = __uint_as_float(r[j]);
-        finish_columns(a, t, z, row0, col, stg, lane);
+        for (int j = 0; j < 8; ++j) z[j] = f32x2_bits(r[2 * j], r[2 * j + 1]);
+        finish_columns(a, t, z, res, row0, col0 + c, cols + c, stg, put, lane);
+        if (!t.vec8) {
+          put += 16;
+          if (put == room || c + 16 >= n) {
+            write_rows(a, row0, col0 + c + 16 - put, min(put, n - (c + 16 - put)), stg, lane);
+            put = 0;
+          }
+        }
         __syncwarp();
       }
       tc_fence_before();
@@ -288,7 +355,7 @@ linear_umma_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
       tc_fence_after();
       float* sums = reinterpret_cast<float*>(smem_gen);
 #pragma unroll 1
-      for (int c = part * 16; c < t.bn; c += 32) {
+      for (int c = part * 16; c < t.bn; c += 16 * kLinParts) {
         uint32_t r[16];
         tmem_ld_32x32b_x16(tmem_base + (uint32_t(q * 32) << 16) + c, r);
         tmem_wait_ld();
@@ -303,28 +370,44 @@ linear_umma_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
     cluster_sync();
     if (warp >= kLinEpiFirst) {
       const int q = warp & 3, part = (warp - kLinEpiFirst) >> 2;
-      float* stg = staging + (warp - kLinEpiFirst) * 32 * kLinPitch;
+      uint32_t* stg = staging + (warp - kLinEpiFirst) * 32 * kLinPitch;
+      float* cols = column_data + (warp - kLinEpiFirst) * 128;
+      const int room = a.out_f32 ? 32 : 64;
       int mt, nt;
       linear_item(t, worker, mt, nt);
       const int64_t row0 = int64_t(mt) * 128 + q * 32;
       const int w = t.bn / t.splits;               // columns this CTA finishes, a multiple of 16
+      const int share = (w / kLinParts + 15) & ~15;
+      const int first = (int)rank * w + part * share;
+      const int64_t col0 = int64_t(nt) * t.bn + first;
+      const int n = row0 < a.T ? (int)max(int64_t(0), min(int64_t(min(share, w - part * share)), a.N - col0)) : 0;
+      if (n > 0) load_columns(a, col0, n, cols, lane);
+      int put = 0;
 #pragma unroll 1
-      for (int c = (int)rank * w + part * 16; c < ((int)rank + 1) * w; c += 32) {
-        const int64_t col = int64_t(nt) * t.bn + c;
-        if (row0 >= a.T || col >= a.N) continue;
-        float z[16];
+      for (int c = 0; c < n; c += 16) {
+        uint4 res[2];
+        load_residual(a, t, row0 + lane, col0 + c, res);
+        uint64_t z[8];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) z[j] = 0.0f;
+        for (int j = 0; j < 8; ++j) z[j] = 0ull;
         for (int s = 0; s < t.splits; ++s) {
-          const uint32_t src = map_to_rank(smem_base + uint32_t(c * 128 + q * 32 + lane) * 4, s);
+          const uint32_t src = map_to_rank(smem_base + uint32_t((first + c) * 128 + q * 32 + lane) * 4, s);
 #pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            float v;
-            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(src + j * 512) : "memory");
-            z[j] += v;
+          for (int j = 0; j < 8; ++j) {
+            float lo, hi;
+            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(lo) : "r"(src + j * 1024) : "memory");
+            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(hi) : "r"(src + j * 1024 + 512) : "memory");
+            z[j] = add_f32x2(z[j], f32x2(lo, hi));
           }
         }
-        finish_columns(a, t, z, row0, col, stg, lane);
+        finish_columns(a, t, z, res, row0, col0 + c, cols + c, stg, put, lane);
+        if (!t.vec8) {
+          put += 16;
+          if (put == room || c + 16 >= n) {
+            write_rows(a, row0, col0 + c + 16 - put, min(put, n - (c + 16 - put)), stg, lane);
+            put = 0;
+          }
+        }
         __syncwarp();
       }
     }
@@ -423,8 +506,8 @@ mote_status_t launch_linear_umma(const LinearArgs& a, cudaStream_t stream) {
   // the smaller operand's tiles change fastest: its whole stays in L2, the larger one is read from HBM once
   t.rows_fast = a.T <= a.N;
   t.a_rows = f.cg == 1 ? (int)std::min<int64_t>(128, (a.T + 7) / 8 * 8) : 128;
-  t.stages = std::min(kLinMaxStages, kLinPipeBytes / (kLinStageA + f.bn / f.cg * 128));
   t.vec8 = a.N % 8 == 0 && (!a.res || a.ldr % 8 == 0);
+  t.stages = std::min(kLinMaxStages, (t.vec8 ? kLinPipeBytes : kLinPipeBytesOdd) / (kLinStageA + f.bn / f.cg * 128));
   t.wide = a.N % 16 == 0 && (reinterpret_cast<uintptr_t>(a.out) & 31u) == 0;
   CUtensorMap ta, tb;
   if (!make_operand_map(&ta, a.x, a.T, a.K, a.ldx, t.a_rows) || !make_operand_map(&tb, a.W, a.N, a.K, a.K, f.bn / f.cg)) return MOTE_ERR_CUDA;
