@@ -14,15 +14,11 @@
 
 namespace mote {
 
-__device__ __forceinline__ uint4 ldg_once(const void* p) {
-  uint4 v;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-  return v;
-}
-__device__ __forceinline__ uint2 ldg_once8(const void* p) {
-  uint2 v;
-  asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
-  return v;
+// kBytes from global into shared memory, behind the thread's back; HBM is asked for whole 128-byte lines.
+template <int kBytes>
+__device__ __forceinline__ void cp_async(uint32_t dst, const void* src) {
+  if (kBytes == 16) asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+  else asm volatile("cp.async.ca.shared.global.L2::128B [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile(
@@ -31,126 +27,182 @@ __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-constexpr int kStreamWarps = 8;
 constexpr int kStreamRows = 16;
+
+// What a warp has in flight: a ring of steps in shared memory, filled by asynchronous copies of its own lanes.  A step's units of 16 bytes
+// per lane: the weights of rows g and g + 8 (INT4: 8 bytes of each in one unit), and the tokens of each column tile, one unit with bf16
+// weights, two with codes, which have twice as many elements to a step.
+template <int NT, int kBits, int kWarps>
+struct StreamRing {
+  static constexpr int kXUnits = kBits == 16 ? 1 : 2;
+  static constexpr int kWUnits = kBits == 4 ? 1 : 2;
+  static constexpr int kUnits = kWUnits + NT * kXUnits;
+  static constexpr int kDepth = kUnits <= 3 ? 8 : kUnits <= 4 ? 6 : 4;     // 8 warps: 96 KB or less, two CTAs per SM
+  static constexpr int kBytes = kWarps * kDepth * kUnits * 32 * 16;
+};
 
 // kBits: storage of W.  A step covers 32 (bf16), 64 (INT8) or 64 (INT4, 32 code bytes) elements of K: lane (g, t) = (lane / 4, lane % 4)
 // takes elements [step * kStep + t * kLane, + kLane) of weight rows g and g + 8 and of its token column; the reduction index may be
-// permuted as long as both operands are.
-template <int NT, int kBits>
-__global__ void __launch_bounds__(kStreamWarps * 32) linear_stream_kernel(LinearArgs a) {
+// permuted as long as both operands are.  The CTA walks over its row tiles, and the ring runs on from one to the next.
+template <int NT, int kBits, int kWarps>
+__global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) linear_stream_kernel(LinearArgs a, int n_tiles) {
+  using R = StreamRing<NT, kBits, kWarps>;
   constexpr int kLane = kBits == 16 ? 8 : 16, kStep = 4 * kLane;
-  constexpr int kAhead = 4;
-  __shared__ float s_part[kStreamWarps][NT * 4][32];
+  extern __shared__ __align__(16) uint8_t s_dyn[];
+  __shared__ float s_part[2][kWarps][NT * 4][32];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const unsigned row_tiles = unsigned((a.N + kStreamRows - 1) / kStreamRows);
-  const int64_t n0 = int64_t(blockIdx.x % row_tiles) * kStreamRows;
-  const int64_t t0 = int64_t(blockIdx.x / row_tiles) * (NT * 8);
   const int n_steps = (a.K + kStep - 1) / kStep;
-  const int sb = n_steps * warp / kStreamWarps, se = n_steps * (warp + 1) / kStreamWarps;
+  const int sb = n_steps * warp / kWarps, n = n_steps * (warp + 1) / kWarps - sb;      // this warp's steps
   const int64_t row_bytes = int64_t(a.K) * kBits / 8;
-  const uint8_t* wa = static_cast<const uint8_t*>(a.W) + min(n0 + g, a.N - 1) * row_bytes + t * (kLane * kBits / 8);
-  const uint8_t* wb = static_cast<const uint8_t*>(a.W) + min(n0 + g + 8, a.N - 1) * row_bytes + t * (kLane * kBits / 8);
+  const uint8_t* w0 = static_cast<const uint8_t*>(a.W) + (sb * kStep + t * kLane) * kBits / 8;
+  // With two units a step, a copy takes the four neighbouring units u * 4 + t of a token's eight, 64 bytes in a row (as each lane's own two
+  // they would be every other 16 bytes, twice the traffic: 8 x 2048 x 11008, INT8: 13.5 us).  Unit c of token g is kept at c ^ (g & 1), where
+  // neither copies nor reads have bank conflicts.
   const uint16_t* tok[NT];
 #pragma unroll
-  for (int n = 0; n < NT; ++n) tok[n] = t0 + n * 8 + g < a.T ? a.x + (t0 + n * 8 + g) * a.ldx + t * kLane : nullptr;
-  // 16 bytes of a weight row, or 8 where they hold the lane's 16 four-bit codes
-  auto load_w = [&](const uint8_t* row, int s) {
-    uint4 v = make_uint4(0u, 0u, 0u, 0u);
-    if (kBits == 4) v = make_uint4(0x88888888u, 0x88888888u, 0u, 0u);      // codes of weight 0
-    if (s < se && s * kStep + t * kLane < a.K) {
-      if (kBits == 4) {
-        const uint2 h = ldg_once8(row + s * (kStep / 2));
-        v.x = h.x; v.y = h.y;
-      } else {
-        v = ldg_once(row + int64_t(s) * (kStep * kBits / 8));
-      }
-    }
-    return v;
+  for (int j = 0; j < NT; ++j) tok[j] = j * 8 + g < a.T ? a.x + (j * 8 + g) * a.ldx + sb * kStep + t * 8 : nullptr;
+  auto x_unit = [&](int j, int c) {              // where unit c of the lane's token is, in units of 16 bytes from the place's start
+    return (R::kWUnits + j * R::kXUnits) * 32 + (R::kXUnits == 1 ? g * 4 + c : g * 8 + (c ^ (g & 1)));
   };
-  float acc[NT][4];
-#pragma unroll
-  for (int n = 0; n < NT; ++n) acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.0f;
+  const int warp_base = warp * (R::kDepth * R::kUnits * 32);
+  const uint4* ring = reinterpret_cast<const uint4*>(s_dyn) + warp_base;
+  const uint32_t ring_addr = (uint32_t)__cvta_generic_to_shared(s_dyn) + warp_base * 16;
   pdl_wait();
   if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = 0u;
-  uint4 qa[kAhead], qb[kAhead];
+
+  // the step that is fetched next: its tile, its number in the warp's share, its place, its rows
+  int f_tile = n > 0 ? (int)blockIdx.x : n_tiles, f_step = 0, f_place = 0;
+  const uint8_t *fa = nullptr, *fb = nullptr;
+  auto fetch = [&]() {
+    if (f_tile < n_tiles) {
+      if (f_step == 0) {
+        const int64_t row = int64_t(f_tile) * kStreamRows + g;
+        fa = w0 + min(row, a.N - 1) * row_bytes;
+        fb = w0 + min(row + 8, a.N - 1) * row_bytes;
+      }
+      const uint32_t dst = ring_addr + f_place * (R::kUnits * 512);
+      const int k0 = (sb + f_step) * kStep;
+      if (k0 + t * kLane < a.K) {
+        if (kBits == 4) {
+          cp_async<8>(dst + lane * 16, fa);
+          cp_async<8>(dst + lane * 16 + 8, fb);
+        } else {
+          cp_async<16>(dst + lane * 16, fa);
+          cp_async<16>(dst + lane * 16 + 512, fb);
+        }
+      }
 #pragma unroll
-  for (int i = 0; i < kAhead; ++i) { qa[i] = load_w(wa, sb + i); qb[i] = load_w(wb, sb + i); }
-  for (int s0 = sb; s0 < se; s0 += kAhead) {
+      for (int j = 0; j < NT; ++j)
+        if (tok[j])
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      const int s = s0 + i;
-      if (s < se) {
-        const uint4 ca = qa[i], cb = qb[i];
-        qa[i] = load_w(wa, s + kAhead);
-        qb[i] = load_w(wb, s + kAhead);
-        const bool in = s * kStep + t * kLane < a.K;
+          for (int u = 0; u < R::kXUnits; ++u)
+            if (k0 + (u * 4 + t) * 8 < a.K) cp_async<16>(dst + x_unit(j, u * 4 + t) * 16, tok[j] + f_step * kStep + u * 32);
+      fa += kStep * kBits / 8;
+      fb += kStep * kBits / 8;
+      if (++f_step == n) { f_step = 0; f_tile += gridDim.x; }
+      f_place = f_place + 1 == R::kDepth ? 0 : f_place + 1;
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          uint4 x0 = make_uint4(0u, 0u, 0u, 0u), x1 = x0;
-          if (tok[n] && in) {
-            const uint4* xp = reinterpret_cast<const uint4*>(tok[n] + s * kStep);
-            x0 = xp[0];
-            if (kBits != 16) x1 = xp[1];
-          }
-          if (kBits == 16) {
-            mma_16816(acc[n], ca.x, cb.x, ca.y, cb.y, x0.x, x0.y);
-            mma_16816(acc[n], ca.z, cb.z, ca.w, cb.w, x0.z, x0.w);
-          } else {
-            const uint32_t xw[8] = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w};
-            uint32_t ea[8], eb[8];
-            if (kBits == 8) {
-              const uint32_t pa[4] = {ca.x, ca.y, ca.z, ca.w}, pb[4] = {cb.x, cb.y, cb.z, cb.w};
+  for (int i = 0; i < R::kDepth - 1; ++i) fetch();
+  // The output that this thread finishes: rows fastest, so that a token's 16 outputs leave together.  Value i of token tile j at lane
+  // (g, t) is weight row g + 8 * (i / 2), token 8j + 2t + (i & 1).
+  const int row = threadIdx.x & 15, token = threadIdx.x >> 4;
+  const bool mine = token < NT * 8 && token < a.T;
+  const int v = ((token >> 3) % NT) * 4 + (row >> 3) * 2 + (token & 1), l = (row & 7) * 4 + ((token & 7) >> 1);
+  static_assert(kWarps * 32 >= NT * 8 * kStreamRows, "an output per thread");
+  int place = 0, buf = 0;
+  for (int tile = blockIdx.x; tile < n_tiles; tile += gridDim.x, buf ^= 1) {
+    const int64_t nn = int64_t(tile) * kStreamRows + row;
+    float scale = 1.0f, bias = 0.0f, res = 0.0f;   // on their way while the products are formed
+    if (mine && nn < a.N) {
+      if (kBits != 16) scale = a.w_scale[nn];
+      if (a.bias) bias = a.bias[nn];
+      if (a.res) res = __uint_as_float(uint32_t(a.res[token * a.ldr + nn]) << 16);
+    }
+    float acc[NT][4];
 #pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                s8x4_to_bf16x2(pa[j], ea[2 * j], ea[2 * j + 1]);
-                s8x4_to_bf16x2(pb[j], eb[2 * j], eb[2 * j + 1]);
-              }
-            } else {
-              uint32_t h[4];
-              u4x8_to_bf16x2(ca.x, h); ea[0] = h[0]; ea[1] = h[1]; ea[2] = h[2]; ea[3] = h[3];
-              u4x8_to_bf16x2(ca.y, h); ea[4] = h[0]; ea[5] = h[1]; ea[6] = h[2]; ea[7] = h[3];
-              u4x8_to_bf16x2(cb.x, h); eb[0] = h[0]; eb[1] = h[1]; eb[2] = h[2]; eb[3] = h[3];
-              u4x8_to_bf16x2(cb.y, h); eb[4] = h[0]; eb[5] = h[1]; eb[6] = h[2]; eb[7] = h[3];
-            }
+    for (int j = 0; j < NT; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.0f;
+    for (int s = 0; s < n; ++s) {
+      __syncwarp();                              // all lanes have read the place that is filled now
+      fetch();
+      asm volatile("cp.async.wait_group %0;" ::"n"(R::kDepth - 1) : "memory");
+      __syncwarp();                              // and all lanes' copies of this step have landed
+      const uint4* at = ring + place * (R::kUnits * 32);
+      place = place + 1 == R::kDepth ? 0 : place + 1;
+      const bool in = (sb + s) * kStep + t * kLane < a.K;                  // places that no copy filled hold anything
+      const uint4 kZero = make_uint4(0u, 0u, 0u, 0u);
+      const uint4 ca = in ? at[lane] : kZero, cb = in && R::kWUnits > 1 ? at[lane + 32] : kZero;
+      uint32_t ea[8], eb[8];
+      if (kBits == 8) {
+        const uint32_t pa[4] = {ca.x, ca.y, ca.z, ca.w}, pb[4] = {cb.x, cb.y, cb.z, cb.w};
 #pragma unroll
-            for (int j = 0; j < 4; ++j) mma_16816(acc[n], ea[2 * j], eb[2 * j], ea[2 * j + 1], eb[2 * j + 1], xw[2 * j], xw[2 * j + 1]);
-          }
+        for (int j = 0; j < 4; ++j) {
+          s8x4_to_bf16x2(pa[j], ea[2 * j], ea[2 * j + 1]);
+          s8x4_to_bf16x2(pb[j], eb[2 * j], eb[2 * j + 1]);
+        }
+      } else if (kBits == 4) {
+        const uint32_t p[4] = {ca.x, ca.y, ca.z, ca.w};                    // two words of row g, two of row g + 8
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          uint32_t h[4];
+          u4x8_to_bf16x2(p[j], h);
+          ea[4 * j] = h[0]; ea[4 * j + 1] = h[1]; ea[4 * j + 2] = h[2]; ea[4 * j + 3] = h[3];
+          u4x8_to_bf16x2(p[2 + j], h);
+          eb[4 * j] = h[0]; eb[4 * j + 1] = h[1]; eb[4 * j + 2] = h[2]; eb[4 * j + 3] = h[3];
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        const bool live = in && tok[j];
+        const uint4 x0 = live ? at[x_unit(j, R::kXUnits * t)] : kZero;
+        if (kBits == 16) {
+          mma_16816(acc[j], ca.x, cb.x, ca.y, cb.y, x0.x, x0.y);
+          mma_16816(acc[j], ca.z, cb.z, ca.w, cb.w, x0.z, x0.w);
+        } else {
+          const uint4 x1 = live ? at[x_unit(j, R::kXUnits * t + R::kXUnits - 1)] : kZero;
+          const uint32_t xw[8] = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) mma_16816(acc[j], ea[2 * i], eb[2 * i], ea[2 * i + 1], eb[2 * i + 1], xw[2 * i], xw[2 * i + 1]);
         }
       }
     }
-  }
+    // the warps' sums meet; two buffers, so that one barrier a tile is enough
 #pragma unroll
-  for (int n = 0; n < NT; ++n)
+    for (int j = 0; j < NT; ++j)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) s_part[warp][n * 4 + i][lane] = acc[n][i];
-  __syncthreads();
-  // value i of token tile n at lane (g, t) is weight row g + 8 * (i / 2), token 8n + 2t + (i & 1); thread -> (token, row) with
-  // the rows fastest, so that a token's 16 outputs leave together
-  for (int o = threadIdx.x; o < NT * 8 * kStreamRows; o += kStreamWarps * 32) {
-    const int row = o & 15, token = o >> 4;
-    const int v = (token >> 3) * 4 + (row >> 3) * 2 + (token & 1), l = (row & 7) * 4 + ((token & 7) >> 1);
-    const int64_t tt = t0 + token, nn = n0 + row;
-    if (tt >= a.T || nn >= a.N) continue;
-    float z = s_part[0][v][l];
+      for (int i = 0; i < 4; ++i) s_part[buf][warp][j * 4 + i][lane] = acc[j][i];
+    __syncthreads();
+    if (mine && nn < a.N) {
+      float z = s_part[buf][0][v][l];
 #pragma unroll
-    for (int w = 1; w < kStreamWarps; ++w) z += s_part[w][v][l];
-    if (kBits != 16) z *= a.w_scale[nn];
-    if (a.bias) z += a.bias[nn];
-    z = apply_act(z, a.act);
-    if (a.res) z += __uint_as_float(uint32_t(a.res[tt * a.ldr + nn]) << 16);
-    if (a.out_f32) static_cast<float*>(a.out)[tt * a.N + nn] = z;
-    else static_cast<uint16_t*>(a.out)[tt * a.N + nn] = (uint16_t)(pack_bf16x2(z, 0.0f) & 0xFFFFu);
+      for (int w = 1; w < kWarps; ++w) z += s_part[buf][w][v][l];
+      if (kBits != 16) z *= scale;
+      z = apply_act(z + bias, a.act) + res;
+      if (a.out_f32) static_cast<float*>(a.out)[token * a.N + nn] = z;
+      else static_cast<uint16_t*>(a.out)[token * a.N + nn] = (uint16_t)(pack_bf16x2(z, 0.0f) & 0xFFFFu);
+    }
   }
 }
 
+template <int NT, int kBits, int kWarps>
+static cudaError_t launch_stream_as(const LinearArgs& a, int tiles, cudaStream_t stream) {
+  static PerDeviceOnce once;
+  constexpr int smem = StreamRing<NT, kBits, kWarps>::kBytes;
+  const cudaError_t e = set_max_dynamic_smem(once, linear_stream_kernel<NT, kBits, kWarps>, smem);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(linear_stream_kernel<NT, kBits, kWarps>, dim3(std::min(tiles, device_sm_count() * (16 / kWarps))), dim3(kWarps * 32), smem, stream,
+                    a, tiles);
+}
+template <int NT, int kBits>
+static cudaError_t launch_stream_bits(const LinearArgs& a, cudaStream_t stream) {
+  const int tiles = (int)((a.N + kStreamRows - 1) / kStreamRows);
+  return tiles <= device_sm_count() ? launch_stream_as<NT, kBits, 16>(a, tiles, stream) : launch_stream_as<NT, kBits, 8>(a, tiles, stream);
+}
 template <int NT>
 static cudaError_t launch_stream(const LinearArgs& a, int bits, cudaStream_t stream) {
-  const dim3 grid((unsigned)((a.N + kStreamRows - 1) / kStreamRows * ((a.T + NT * 8 - 1) / (NT * 8))));
-  const dim3 block(kStreamWarps * 32);
-  return bits == 16  ? launch_pdl(linear_stream_kernel<NT, 16>, grid, block, 0, stream, a)
-         : bits == 8 ? launch_pdl(linear_stream_kernel<NT, 8>, grid, block, 0, stream, a)
-                     : launch_pdl(linear_stream_kernel<NT, 4>, grid, block, 0, stream, a);
+  return bits == 16 ? launch_stream_bits<NT, 16>(a, stream) : bits == 8 ? launch_stream_bits<NT, 8>(a, stream) : launch_stream_bits<NT, 4>(a, stream);
 }
 
 // RTN codes -> the same integers as bf16, for the tensor-core product; 8 code bytes per thread and step.

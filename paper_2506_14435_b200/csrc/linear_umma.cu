@@ -17,6 +17,7 @@
 #include <cuda.h>
 
 #include <algorithm>
+#include <atomic>
 #include <mutex>
 
 #include "linear_act.cuh"
@@ -455,23 +456,26 @@ static bool make_operand_map(CUtensorMap* m, const void* base, int64_t rows, int
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Which form and tile width: the least estimated time, in cycles.
+// Which form and tile width: the least estimated time, in cycles.  The estimate's constants were fitted to times of all forms at 70
+// sizes (17 to 8192 tokens, 26 to 11008 rows, K 128 to 11008): the form that it names is 2.5 % slower than the best one on average and
+// 24 % at worst; 4096 x 11008 x 2048: pairs of 256 x 224, 126 us (single CTAs 136), 333 x 8960 x 1536: single CTAs of 192, 13 us (pairs
+// 16), 64 x 2048 x 2048: tiles of 64 split four ways, 8.5 us (whole 12).
 struct LinearForm { int cg, bn, splits; };
-static LinearForm pick_form(int64_t T, int64_t N, int k_steps, int sms) {
+static LinearForm pick_form(int64_t T, int64_t N, int k_steps, int sms, const int (&clusters)[9]) {
   LinearForm best{1, 256, 1};
   double best_cost = 1e300;
   auto consider = [&](int cg, int bn, int splits) {
     const int64_t items = ((T + 128 * cg - 1) / (128 * cg)) * ((N + bn - 1) / bn);
-    const int64_t workers = std::max(1, sms / (cg * splits));
-    const int64_t rounds = (items + workers - 1) / workers;
+    const int64_t workers = splits > 1 ? clusters[splits] : sms / cg;            // items that are worked on at a time
+    if (workers < 1) return;
+    const double rounds = double((items + workers - 1) / workers);
     const double active = double(std::min(items, workers)) * cg * splits;
-    // a step: four MMAs, or the way of its operands from L2 (some 6 KB a cycle for all SMs, 64 bytes for one)
-    const double rows = std::min<int64_t>(T, 128);
-    const double bytes = rows * 128 + double(bn / cg) * 128;
-    const double step = std::max({2.0 * std::max(bn, 64), bytes / 64.0, bytes * active / 6000.0});
-    const int steps = (k_steps + splits - 1) / splits;
-    const double epilogue = 6.0 * bn / splits + (splits > 1 ? 1500.0 + 4.0 * bn : 0.0);
-    const double cost = double(rounds) * steps * step + epilogue + (rounds > 1 ? 200.0 * rounds : 0.0);
+    // a step: four MMAs, the way of its operands from L2 (77 bytes a cycle for an SM, 9300 for all of them), or a stage's latency
+    const double bytes = double(std::min<int64_t>(T, 128)) * 128 + double(bn / cg) * 128;
+    const double step = std::max({2.0 * bn, bytes / 77.0, bytes * active / 9300.0, 420.0});
+    const double main = double((k_steps + splits - 1) / splits) * step;
+    const double epilogue = 2000.0 + 24.0 * bn / splits + (splits > 1 ? 4700.0 + 23.0 * bn : 0.0);
+    const double cost = main + epilogue + (rounds - 1) * (std::max(main, epilogue) + 1000.0);
     if (cost < best_cost) { best_cost = cost; best = {cg, bn, splits}; }
   };
   const int bn_max = (int)std::min<int64_t>(256, (N + 15) / 16 * 16);
@@ -483,6 +487,33 @@ static LinearForm pick_form(int64_t T, int64_t N, int k_steps, int sms) {
     for (int bn = 16 * splits; bn <= 256; bn += 16 * splits)
       if (k_steps >= 2 * splits && bn - 16 * splits < N) consider(1, bn, splits);
   return best;
+}
+
+// Clusters of 2, 4 and 8 CTAs of the split form that the current device runs at a time (an SM takes one CTA; how many clusters that makes
+// depends on how its SMs are grouped: 74, 33 and 15 on a B200 of 148).  0 where the query fails.
+static void resident_clusters(int (&clusters)[9]) {
+  static std::atomic<int> cache[kMaxDevices][9];
+  const int dev = current_device();
+  for (int c = 2; c <= 8; c *= 2) {
+    int n = dev >= 0 && dev < kMaxDevices ? cache[dev][c].load(std::memory_order_relaxed) : 0;
+    if (n == 0) {
+      cudaLaunchConfig_t cfg = {};
+      cfg.gridDim = dim3(c);
+      cfg.blockDim = dim3(kLinThreads);
+      cfg.dynamicSmemBytes = kLinSmem;
+      cudaLaunchAttribute attr[1];
+      attr[0].id = cudaLaunchAttributeClusterDimension;
+      attr[0].val.clusterDim.x = (unsigned)c;
+      attr[0].val.clusterDim.y = 1;
+      attr[0].val.clusterDim.z = 1;
+      cfg.attrs = attr;
+      cfg.numAttrs = 1;
+      if (cudaOccupancyMaxActiveClusters(&n, linear_umma_kernel<1, true>, &cfg) != cudaSuccess) { (void)cudaGetLastError(); n = 0; }
+      n = n > 0 ? n : -1;
+      if (dev >= 0 && dev < kMaxDevices) cache[dev][c].store(n, std::memory_order_relaxed);
+    }
+    clusters[c] = n;
+  }
 }
 
 template <int CG, bool kSplit>
@@ -498,7 +529,11 @@ mote_status_t launch_linear_umma(const LinearArgs& a, cudaStream_t stream) {
   const int sms = device_sm_count();
   LinearTiles t{};
   t.k_steps = (a.K + 63) / 64;
-  const LinearForm f = pick_form(a.T, a.N, t.k_steps, sms);
+  static PerDeviceOnce split_once;               // its shared-memory limit has to be set before the query
+  if (set_max_dynamic_smem(split_once, linear_umma_kernel<1, true>, kLinSmem) != cudaSuccess) return MOTE_ERR_CUDA;
+  int clusters[9] = {};
+  resident_clusters(clusters);
+  const LinearForm f = pick_form(a.T, a.N, t.k_steps, sms, clusters);
   t.bn = f.bn; t.splits = f.splits;
   t.n_mt = (int)((a.T + 128 * f.cg - 1) / (128 * f.cg));
   t.n_nt = (int)((a.N + f.bn - 1) / f.bn);
