@@ -204,7 +204,8 @@ mote_status_t mote_route_stats(const float* logits, const int32_t* topk_idx, int
  * logit_bias and select_bias may hold -inf: such an expert is chosen only where fewer than k others are left.
  *
  *   Wr      [E, d], w_dtype MOTE_DTYPE_F32 or MOTE_DTYPE_BF16, 16-B aligned; logit_bias, select_bias [E] float or NULL
- *   packed  output of mote_router_pack for this Wr, 256-B aligned
+ *   packed  output of mote_router_pack for this Wr, 256-B aligned; its first word is the device status of
+ *           mote_device_status, which stays until it is read
  *   x_bf16  in   [T, d] bf16, row stride ldx elements (ldx >= d, ldx % 8 == 0), 16-B aligned
  *   topk_idx out [T, k] int32;  topk_w out [T, k] float;  logits out [T, E] float or NULL
  * T = 0 is a no-op.  Errors: d % 8 != 0, d > 32768, E < 1, E > MOTE_MAX_EXPERTS, k < 1, k > E, k > MOTE_MAX_TOPK, n_groups not

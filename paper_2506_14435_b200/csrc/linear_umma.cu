@@ -14,14 +14,11 @@
 //                            distributed shared memory, are added in rank order, and each CTA finishes its share of the columns
 //
 // Every mbarrier wait is bounded; on expiry the CTA raises the status word and leaves.
-#include <cuda.h>
-
 #include <algorithm>
-#include <atomic>
-#include <mutex>
 
 #include "linear_act.cuh"
 #include "ptx_sm100.cuh"
+#include "tile_launch.cuh"
 
 namespace mote {
 
@@ -434,28 +431,6 @@ linear_umma_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
 // ------------------------------------------------------------------------------------------------
 // Host side
 // ------------------------------------------------------------------------------------------------
-using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                              const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-// bf16 [rows, cols] with a row stride in elements; box [box_rows, 64], 128-byte swizzle
-static bool make_operand_map(CUtensorMap* m, const void* base, int64_t rows, int64_t cols, int64_t stride, int box_rows) {
-  static EncodeFn fn = nullptr;
-  static std::once_flag once;
-  std::call_once(once, [] {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess)
-      fn = reinterpret_cast<EncodeFn>(p);
-  });
-  if (!fn) return false;
-  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
-  const cuuint64_t strides[1] = {(cuuint64_t)stride * 2};
-  const cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
-  const cuuint32_t estr[2] = {1, 1};
-  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 // Which form and tile width: the least estimated time, in cycles.  The estimate's constants were fitted to times of all forms at 70
 // sizes (17 to 8192 tokens, 26 to 11008 rows, K 128 to 11008): the form that it names is 2.5 % slower than the best one on average and
 // 24 % at worst; 4096 x 11008 x 2048: pairs of 256 x 224, 126 us (single CTAs 136), 333 x 8960 x 1536: single CTAs of 192, 13 us (pairs
@@ -489,33 +464,6 @@ static LinearForm pick_form(int64_t T, int64_t N, int k_steps, int sms, const in
   return best;
 }
 
-// Clusters of 2, 4 and 8 CTAs of the split form that the current device runs at a time (an SM takes one CTA; how many clusters that makes
-// depends on how its SMs are grouped: 74, 33 and 15 on a B200 of 148).  0 where the query fails.
-static void resident_clusters(int (&clusters)[9]) {
-  static std::atomic<int> cache[kMaxDevices][9];
-  const int dev = current_device();
-  for (int c = 2; c <= 8; c *= 2) {
-    int n = dev >= 0 && dev < kMaxDevices ? cache[dev][c].load(std::memory_order_relaxed) : 0;
-    if (n == 0) {
-      cudaLaunchConfig_t cfg = {};
-      cfg.gridDim = dim3(c);
-      cfg.blockDim = dim3(kLinThreads);
-      cfg.dynamicSmemBytes = kLinSmem;
-      cudaLaunchAttribute attr[1];
-      attr[0].id = cudaLaunchAttributeClusterDimension;
-      attr[0].val.clusterDim.x = (unsigned)c;
-      attr[0].val.clusterDim.y = 1;
-      attr[0].val.clusterDim.z = 1;
-      cfg.attrs = attr;
-      cfg.numAttrs = 1;
-      if (cudaOccupancyMaxActiveClusters(&n, linear_umma_kernel<1, true>, &cfg) != cudaSuccess) { (void)cudaGetLastError(); n = 0; }
-      n = n > 0 ? n : -1;
-      if (dev >= 0 && dev < kMaxDevices) cache[dev][c].store(n, std::memory_order_relaxed);
-    }
-    clusters[c] = n;
-  }
-}
-
 template <int CG, bool kSplit>
 static cudaError_t launch_form(const CUtensorMap& ta, const CUtensorMap& tb, const LinearArgs& a, const LinearTiles& t, int grid, int cluster,
                                cudaStream_t stream) {
@@ -531,8 +479,9 @@ mote_status_t launch_linear_umma(const LinearArgs& a, cudaStream_t stream) {
   t.k_steps = (a.K + 63) / 64;
   static PerDeviceOnce split_once;               // its shared-memory limit has to be set before the query
   if (set_max_dynamic_smem(split_once, linear_umma_kernel<1, true>, kLinSmem) != cudaSuccess) return MOTE_ERR_CUDA;
+  static ResidentClusters resident;
   int clusters[9] = {};
-  resident_clusters(clusters);
+  for (int c = 2; c <= 8; c *= 2) clusters[c] = resident.get(linear_umma_kernel<1, true>, kLinThreads, kLinSmem, c);
   const LinearForm f = pick_form(a.T, a.N, t.k_steps, sms, clusters);
   t.bn = f.bn; t.splits = f.splits;
   t.n_mt = (int)((a.T + 128 * f.cg - 1) / (128 * f.cg));

@@ -320,7 +320,7 @@ static mote_status_t layer_forward(const mote_layer_t* L, const mote_router_t* R
     if (taps && (!taps->acc_gate != !taps->acc_up)) return MOTE_ERR_NULL;
     mote_status_t st;
     if (R) {                                                  // what the prologue kernel does, step by step
-      st = launch_route_scored(R, x, d, T, topk_idx, topk_w, nullptr, stream);
+      st = launch_route_scored(R, x, d, T, topk_idx, topk_w, nullptr, status, stream);
       if (st) return st;
       st = launch_dispatch(topk_idx, P, E, offsets, perm, inv, stream);
       if (st) return st;
@@ -398,7 +398,7 @@ static mote_status_t layer_forward(const mote_layer_t* L, const mote_router_t* R
   auto* blk_base = reinterpret_cast<int32_t*>(base + pl.blk_base);
   const int n_blk = (int)((T + kRouteBlockTokens - 1) / kRouteBlockTokens);
   if (R) {
-    st = launch_route_scored(R, x, d, T, topk_idx, topk_w, nullptr, stream);
+    st = launch_route_scored(R, x, d, T, topk_idx, topk_w, nullptr, status, stream);
     if (!st && tensor) st = launch_block_counts(topk_idx, T, E, k, blk_hist, stream);
   } else {
     st = launch_route_topk(x, T, d, L->Wr, L->router_bias, E, k, L->norm_topk, topk_idx, topk_w, nullptr,

@@ -48,8 +48,9 @@ mote_status_t launch_route_topk(const void* x, int64_t T, int d, const float* Wr
 
 // Scored router (mote_route_scored); check_router: the argument checks of the calls that take one.
 mote_status_t check_router(const mote_router_t* R);
+// status: the device status word that a bounded wait raises; null: the router's own.
 mote_status_t launch_route_scored(const mote_router_t* R, const void* x, int64_t ldx, int64_t T, int32_t* idx, float* w,
-                                  float* logits, cudaStream_t stream);
+                                  float* logits, uint32_t* status, cudaStream_t stream);
 // blk_hist of launch_route_topk from finished choices.
 mote_status_t launch_block_counts(const int32_t* idx, int64_t T, int E, int k, int32_t* blk_hist, cudaStream_t stream);
 

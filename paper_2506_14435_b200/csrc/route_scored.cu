@@ -11,10 +11,13 @@
 // Logits: one cluster of CTAs per 16 tokens.  Each warp takes a part of the width and multiplies 16 tokens by all experts with
 // warp-level bf16 MMAs; an fp32 router weight is split exactly into three bf16 terms (8 + 8 + 8 significand bits), so every
 // product is exact and only the additions round.  The warps' sums meet in shared memory, the CTAs' in distributed shared
-// memory (in rank order), and each CTA of the cluster then chooses for its share of the 16 tokens, a warp per token.
+// memory (in rank order), and each CTA of the cluster then chooses for its share of the 16 tokens.
+#include <algorithm>
+
 #include "mote_common.cuh"
 #include "mote_internal.h"
 #include "ptx_sm100.cuh"
+#include "tile_launch.cuh"
 
 namespace mote {
 
@@ -31,264 +34,494 @@ struct ScoredRouter {
 };
 
 // ------------------------------------------------------------------------------------------------
-// Error bounds.  A product is exact, so a logit is off by the roundings of its partial sums.  These are no larger than
-// |x|_2 |w|_2 (Cauchy-Schwarz), and the roundings of one sum are a few dozen of 2^-24 of the partial sum each, most of it far
-// below that; kLogitEps |x|_2 |w|_2 is some 50 times what was seen.  (What all experts of a token have in common, as the truncation
-// of the MMA's additions for operands of one sign, cancels in the comparison.)
+// Error bounds.  A product is exact, so a logit is off by the roundings of its partial sums, which are no larger than |x|_2 |w|_2
+// (Cauchy-Schwarz).  An MMA truncates what it adds up, hence sums of one step only (32 or 64 elements of the width) are left to it; they
+// join the others by additions rounded to nearest.  Truncation takes off a part of a logit that is the same for all experts; what is
+// left was at most 2^-22.2 |x|_2 |w|_2 over 10^7 logits of normal, outlier and one-signed tokens, widths 256 to 32768 (rms 2^-25.4 and less).
 // ------------------------------------------------------------------------------------------------
-constexpr float kLogitEps = 9.5367432e-07f;            // 2^-20
+constexpr float kLogitEps = 5.4e-07f;                  // 2^-21, and an eighth for the roundings where sums meet
 
-// order-preserving integer images of floats; never 0, which marks an entry that cannot be taken
+// order-preserving integer images of floats and doubles; never 0, which marks an entry that cannot be taken
 __device__ __forceinline__ uint32_t order_key(float v) {
   const uint32_t b = __float_as_uint(v + 0.0f);          // -0 counts as +0
   const uint32_t k = (b & 0x80000000u) ? ~b : b | 0x80000000u;
   return k ? k : 1u;
 }
+__device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? k & 0x7FFFFFFFu : ~k); }
 __device__ __forceinline__ uint64_t order_key(double v) {
   const uint64_t b = (uint64_t)__double_as_longlong(v + 0.0);
   const uint64_t k = (b >> 63) ? ~b : b | (1ull << 63);
   return k ? k : 1ull;
 }
-template <typename F> struct KeyOf { using type = uint32_t; };
-template <> struct KeyOf<double> { using type = uint64_t; };
-
-__device__ __forceinline__ uint32_t warp_max_key(uint32_t k) { return __reduce_max_sync(0xffffffffu, k); }
-__device__ __forceinline__ uint64_t warp_max_key(uint64_t k) {
-  const uint32_t hi = (uint32_t)(k >> 32);
-  const uint32_t m = __reduce_max_sync(0xffffffffu, hi);
-  const uint32_t lo = __reduce_max_sync(0xffffffffu, hi == m ? (uint32_t)k : 0u);
-  return (uint64_t(m) << 32) | lo;
-}
-
-// The entry with the largest key of 64 (lane, and lane + 32 in the second slot); equal keys: the lower number.  -1 if all are 0.
-template <typename K>
-__device__ __forceinline__ int warp_argmax(K k0, K k1) {
-  const K m = warp_max_key(k0 > k1 ? k0 : k1);
-  if (m == 0) return -1;
-  const unsigned b0 = __ballot_sync(0xffffffffu, k0 == m);
-  if (b0) return __ffs(b0) - 1;
-  return 31 + __ffs(__ballot_sync(0xffffffffu, k1 == m));
-}
-template <typename F>
-__device__ __forceinline__ F entry(F v0, F v1, int e) {
-  const F a = __shfl_sync(0xffffffffu, v0, e & 31), b = __shfl_sync(0xffffffffu, v1, e & 31);
-  return e < 32 ? a : b;
-}
-__device__ __forceinline__ double warp_sum_f(double v) {
+__device__ __forceinline__ double warp_sum_f64(double v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
-__device__ __forceinline__ float warp_sum_f(float v) { return warp_sum(v); }
-__device__ __forceinline__ double warp_max_f(double v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v = fmax(v, __shfl_xor_sync(0xffffffffu, v, o));
-  return v;
-}
-__device__ __forceinline__ float warp_max_f(float v) { return warp_max(v); }
-__device__ __forceinline__ double exp_f(double v) { return exp(v); }
-__device__ __forceinline__ float exp_f(float v) { return expf(v); }
+__device__ __forceinline__ float finite_abs(float v) { return fabsf(v) < INFINITY ? fabsf(v) : 0.0f; }
 
-// Chooses the experts of one token from its logits (a warp; lane holds experts lane and lane + 32; s_c: 64 values of the warp's
-// own) and, unless a score comparison lies within the error bound, writes them.  F = float: `delta` bounds the error of a
-// logit; returned is the set of experts whose logits have to be evaluated again (0: none, the choice stands).  F = double: the
-// logits are exact for that purpose, the choice always stands.
-template <typename F>
-__device__ __forceinline__ uint64_t choose_experts(const ScoredRouter& r, int64_t token, F l0, F l1, float delta, F* s_c, int lane) {
-  using K = typename KeyOf<F>::type;
+// ------------------------------------------------------------------------------------------------
+// The choice from fp32 sums: a warp to a token, experts lane and lane + 32 to a lane.  It is a chain of dependent steps, so its latency counts:
+// maxima are single warp reductions of integer images of the scores.  Loops stay loops: every SM runs through this code a few times
+// only, and fetching it takes time too.  (Four or eight lanes to a token, 16 or 8 experts to a lane: 20 000 cycles a token, and no
+// faster for the 64 tokens that a CTA has in a long batch.)
+// ------------------------------------------------------------------------------------------------
+// The entry with the largest key of 64 (lane, and lane + 32 in the second slot), of equal ones the lower number.  Key 0: none.
+__device__ __forceinline__ int warp_argmax(uint32_t k0, uint32_t k1, uint32_t& best) {
+  best = __reduce_max_sync(0xffffffffu, max(k0, k1));
+  const unsigned b0 = __ballot_sync(0xffffffffu, k0 == best), b1 = __ballot_sync(0xffffffffu, k1 == best);
+  return b0 ? __ffs(b0) - 1 : 31 + __ffs(b1);
+}
+
+// What is known of a token whose choice the fp32 scores leave open.
+struct Doubt {
+  int token;                                       // number within the CTA's tokens
+  int full;                                        // 1: all logits and the whole choice anew
+  int in, out;                                     // the groups on either side of the border, if they are too close; else -1
+  uint64_t which;                                  // experts whose order is open
+  uint64_t settled;                                // experts whose logits are evaluated in 64 bits: those, and the groups' (0: no doubt)
+  uint64_t chosen;                                 // the fp32 choice, six bits each
+};
+
+// What a lane holds of the router: the biases of its two experts, and their largest magnitudes over all experts.
+struct LaneBias {
+  float s0 = 0.0f, s1 = 0.0f, select_max = 0.0f, logit_max = 0.0f;
+  __device__ __forceinline__ void load(const ScoredRouter& r, int lane) {
+    const bool v0 = lane < r.E, v1 = lane + 32 < r.E;
+    float l0 = 0.0f, l1 = 0.0f;
+    if (r.select_bias) {
+      if (v0) s0 = r.select_bias[lane];
+      if (v1) s1 = r.select_bias[lane + 32];
+    }
+    if (r.logit_bias) {
+      if (v0) l0 = r.logit_bias[lane];
+      if (v1) l1 = r.logit_bias[lane + 32];
+    }
+    // (an expert barred by -inf takes no part in the rounding of the others)
+    select_max = warp_max(fmaxf(finite_abs(s0), finite_abs(s1)));
+    logit_max = warp_max(fmaxf(finite_abs(l0), finite_abs(l1)));
+  }
+};
+
+// Chooses for one token (a warp) from its logits l0, l1 (off by up to `delta`) and, unless a comparison lies within the error bound, writes
+// the choice.  s_c: 64 floats of the warp's own.  Returned: in `d` what is in doubt (which = 0: nothing, the choice stands), and the
+// scores of the lane's experts.
+__device__ __forceinline__ void choose_experts(const ScoredRouter& r, const LaneBias& bias, int64_t token, float l0, float l1, float delta,
+                                               float* s_c, Doubt& d, float& p0, float& p1, int lane) {
   const int E = r.E, k = r.k;
   const bool v0 = lane < E, v1 = lane + 32 < E;
-  const F kNone = F(-INFINITY);
-  // scores
-  F p0, p1;
-  F smax = F(1);
-  if (r.sigmoid) {
-    p0 = F(1) / (F(1) + exp_f(-l0));
-    p1 = F(1) / (F(1) + exp_f(-l1));
-  } else {
-    const F lm = warp_max_f(v0 ? (v1 ? (l0 > l1 ? l0 : l1) : l0) : kNone);
-    p0 = v0 ? exp_f(l0 - lm) : F(0);
-    p1 = v1 ? exp_f(l1 - lm) : F(0);
-    const F den = warp_sum_f(p0 + p1);
-    p0 /= den;
-    p1 /= den;
-    smax = F(1) / den;
-  }
-  // what the choice goes by.  Both scores grow with the logit: without a bias and without groups (whose sums need the
-  // scores) the logits themselves are compared.
+  // Both scores grow with the logit: without a bias and without groups (whose sums need the scores) the logits are compared.
   const bool by_logit = !r.select_bias && r.n_groups == 1;
-  F c0 = by_logit ? l0 : p0, c1 = by_logit ? l1 : p1;
-  float bias_max = 0.0f;
-  if (r.select_bias) {
-    const float b0 = v0 ? r.select_bias[lane] : 0.0f, b1 = v1 ? r.select_bias[lane + 32] : 0.0f;
-    c0 += b0;
-    c1 += b1;
-    // an expert barred by -inf takes no part in the rounding of the others
-    bias_max = warp_max(fmaxf(fabsf(b0) < INFINITY ? fabsf(b0) : 0.0f, fabsf(b1) < INFINITY ? fabsf(b1) : 0.0f));
+  float smax = 1.0f;
+  if (r.sigmoid) {
+    p0 = 1.0f / (1.0f + expf(-l0));
+    p1 = 1.0f / (1.0f + expf(-l1));
+  } else {
+    const float lm = warp_max(fmaxf(v0 ? l0 : -INFINITY, v1 ? l1 : -INFINITY));
+    p0 = v0 ? expf(l0 - lm) : 0.0f;
+    p1 = v1 ? expf(l1 - lm) : 0.0f;
+    smax = 1.0f / warp_sum(p0 + p1);
+    p0 *= smax;
+    p1 *= smax;
   }
-  // bound on the error of c: of the logit through the score's slope, of expf and the divisions, of adding the bias
-  float tau = 0.0f;
-  if (sizeof(F) == 4) {
-    tau = by_logit ? delta : r.sigmoid ? 0.25f * delta + 4.8e-7f : float(smax) * (2.0f * delta + 2e-6f);
-    tau += 1.2e-7f * bias_max;
-  }
-  bool doubt_all = false;
-  uint64_t eligible = ~0ull;
+  const float c0 = (by_logit ? l0 : p0) + bias.s0, c1 = (by_logit ? l1 : p1) + bias.s1;
+  // bound on the error of c: of the logit through the score's slope, of expf and the division, of adding the bias
+  const float tau = (by_logit ? delta : r.sigmoid ? 0.25f * delta + 4.8e-7f : smax * (2.0f * delta + 2e-6f)) + 1.2e-7f * bias.select_max;
+  uint32_t k0 = v0 ? order_key(c0) : 0u, k1 = v1 ? order_key(c1) : 0u, best;
+  d.full = 0;
+  d.which = d.settled = 0ull;
+  d.in = d.out = -1;
   if (r.n_groups > 1) {
     const int G = r.n_groups, per = E / G;
     __syncwarp();
-    if (v0) s_c[lane] = c0;
-    if (v1) s_c[lane + 32] = c1;
+    s_c[lane] = c0;
+    s_c[lane + 32] = c1;
     __syncwarp();
-    auto group_score = [&](int g) {
-      F a = s_c[g * per], b = kNone;
-      for (int i = 1; i < per; ++i) {
-        const F v = s_c[g * per + i];
-        if (v > a) { b = a; a = v; }
-        else if (v > b) b = v;
+    uint32_t g0 = 0u, g1 = 0u;                     // keys of groups lane and lane + 32
+    float second0 = 0.0f, second1 = 0.0f;          // the smaller of the scores that they are made of
+#pragma unroll 1
+    for (int g = lane; g < G; g += 32) {
+      float a = s_c[g * per], b = -INFINITY;
+#pragma unroll 4
+      for (int m = 1; m < per; ++m) {
+        const float v = s_c[g * per + m];
+        b = fmaxf(b, fminf(a, v));
+        a = fmaxf(a, v);
       }
-      return per > 1 ? a + b : a;
-    };
-    const F g0 = lane < G ? group_score(lane) : kNone, g1 = lane + 32 < G ? group_score(lane + 32) : kNone;
-    K k0 = lane < G ? order_key(g0) : K(0), k1 = lane + 32 < G ? order_key(g1) : K(0);
-    F last = kNone;
-    eligible = 0ull;
+      const float second = per > 1 ? b : a;
+      const uint32_t key = order_key(per > 1 ? a + b : a);
+      if (g < 32) { g0 = key; second0 = second; } else { g1 = key; second1 = second; }
+    }
+    uint64_t kept = 0ull;
+    uint32_t rest0 = g0, rest1 = g1, last = 0u;
+    int in = 0;
+#pragma unroll 1
     for (int j = 0; j < r.topk_groups; ++j) {
-      const int g = warp_argmax(k0, k1);
-      last = entry(g0, g1, g);
-      if (lane == (g & 31)) { if (g < 32) k0 = K(0); else k1 = K(0); }
-      eligible |= (per == 64 ? ~0ull : ((1ull << per) - 1ull)) << (g * per);
+      in = warp_argmax(rest0, rest1, last);
+      if (lane == in) rest0 = 0u;
+      if (lane + 32 == in) rest1 = 0u;
+      kept |= 1ull << in;
     }
-    if (sizeof(F) == 4) {
-      const int g = warp_argmax(k0, k1);
-      if (g >= 0 && float(last - entry(g0, g1, g)) <= 4.0f * tau + 2.4e-7f * (fabsf(float(last)) < INFINITY ? fabsf(float(last)) : 0.0f))
-        doubt_all = true;
-    }
-  }
-  const bool e0 = v0 && ((eligible >> lane) & 1ull), e1 = v1 && ((eligible >> (lane + 32)) & 1ull);
-  K k0 = e0 ? order_key(c0) : K(0), k1 = e1 ? order_key(c1) : K(0);
-  int sel[MOTE_MAX_TOPK];
-  F sp[MOTE_MAX_TOPK];
-  unsigned m0 = 0u, m1 = 0u;                     // experts in doubt
-  F sum = F(0);
-#pragma unroll
-  for (int j = 0; j < MOTE_MAX_TOPK; ++j) {
-    if (j < k) {
-      const int e = warp_argmax(k0, k1);
-      sel[j] = e;
-      sp[j] = entry(p0, p1, e);
-      sum += sp[j];
-      if (lane == (e & 31)) { if (e < 32) k0 = K(0); else k1 = K(0); }
-      if (sizeof(F) == 4) {
-        // entries still to come that are closer to this one than the errors allow: they and it are in doubt
-        const F ce = entry(c0, c1, e);
-        const unsigned b0 = __ballot_sync(0xffffffffu, k0 != K(0) && float(ce - c0) <= 2.0f * tau);
-        const unsigned b1 = __ballot_sync(0xffffffffu, k1 != K(0) && float(ce - c1) <= 2.0f * tau);
-        if (b0 | b1) {
-          m0 |= b0; m1 |= b1;
-          if (e < 32) m0 |= 1u << e; else m1 |= 1u << (e - 32);
+    if (r.topk_groups < G) {
+      const int out = warp_argmax(rest0, rest1, best);
+      const float worst = key_value(last), reach = 4.0f * tau + 2.4e-7f * finite_abs(worst);
+      if (worst - key_value(best) <= reach) {
+        // The last group that stays and the first one left out are too close.  If they are the only ones at the border, the scores that
+        // their sums may be made of are evaluated; a third group there: everything.
+        const float lo = key_value(best) - reach, hi = worst + reach;
+        auto at_border = [&](uint32_t key) { return key != 0u && key_value(key) >= lo && key_value(key) <= hi; };
+        const int n = __popc(__ballot_sync(0xffffffffu, at_border(g0))) + __popc(__ballot_sync(0xffffffffu, at_border(g1)));
+        if (n > 2) {
+          d.full = 1;
+        } else {
+          d.in = in;
+          d.out = out;
+          const float floor_in = __shfl_sync(0xffffffffu, in < 32 ? second0 : second1, in & 31) - 2.0f * tau;
+          const float floor_out = __shfl_sync(0xffffffffu, out < 32 ? second0 : second1, out & 31) - 2.0f * tau;
+          auto part_of = [&](bool there, int e, float c) { return there && ((e / per == in && c >= floor_in) || (e / per == out && c >= floor_out)); };
+          d.settled = uint64_t(__ballot_sync(0xffffffffu, part_of(v1, lane + 32, c1))) << 32 | __ballot_sync(0xffffffffu, part_of(v0, lane, c0));
         }
       }
     }
+    if (!((kept >> (lane / per)) & 1ull)) k0 = 0u;
+    if (!((kept >> ((lane + 32) / per)) & 1ull)) k1 = 0u;
   }
-  if (sizeof(F) == 4) {
-    const uint64_t all = E == 64 ? ~0ull : (1ull << E) - 1ull;
-    uint64_t doubt = (uint64_t(m1) << 32) | m0;
+  // The k largest.  A lane keeps the place of its experts and the key of the choice before (all choices before an expert's are larger
+  // still, so that one is the closest).
+  int slot0 = k, slot1 = k;
+  uint32_t rest0 = k0, rest1 = k1, prev = 0u, before0 = 0u, before1 = 0u;
+#pragma unroll 1
+  for (int j = 0; j < k; ++j) {
+    const int e = warp_argmax(rest0, rest1, best);
+    if (lane == e) { slot0 = j; before0 = prev; rest0 = 0u; }
+    if (lane + 32 == e) { slot1 = j; before1 = prev; rest1 = 0u; }
+    prev = best;
+  }
+  if (slot0 == k) before0 = prev;
+  if (slot1 == k) before1 = prev;
+  // closer to the choice before than the errors allow?  (key 0: cannot be taken; the first choice has none before it; equal -inf are decided)
+  auto is_near = [&](uint32_t key, int slot, uint32_t before) {
+    const float c = key_value(key);
+    return key != 0u && slot > 0 && c > -INFINITY && key_value(before) - c <= 2.0f * tau;
+  };
+  const bool near0 = is_near(k0, slot0, before0), near1 = is_near(k1, slot1, before1);
+  if (__any_sync(0xffffffffu, near0 || near1) || d.full || d.in >= 0) {
+    // those experts, and the choices before them
+    uint64_t which = uint64_t(__ballot_sync(0xffffffffu, near1)) << 32 | __ballot_sync(0xffffffffu, near0), chosen = 0ull;
+    const unsigned places = __reduce_or_sync(0xffffffffu, (near0 ? 1u << (slot0 - 1) : 0u) | (near1 ? 1u << (slot1 - 1) : 0u));
+#pragma unroll 1
+    for (int j = 0; j < k; ++j) {
+      const unsigned b0 = __ballot_sync(0xffffffffu, slot0 == j), b1 = __ballot_sync(0xffffffffu, slot1 == j);
+      const int e = b0 ? __ffs(b0) - 1 : 31 + __ffs(b1);
+      chosen |= uint64_t(e) << (6 * j);
+      if ((places >> j) & 1u) which |= 1ull << e;
+    }
+    d.chosen = chosen;
+    d.which = which;
     // scores of a softmax share their denominator: exact differences need every logit
-    if (doubt_all || (doubt && !r.sigmoid && !by_logit)) doubt = all;
-    if (doubt) return doubt & all;
+    if (!r.sigmoid && !by_logit) d.full = 1;
+    d.settled = d.full ? (E == 64 ? ~0ull : (1ull << E) - 1ull) : d.settled | which;
+    return;
   }
-  if (lane == 0) {
-    const F div = r.renorm ? (sum > F(1e-20) ? sum : F(1e-20)) : F(1);
-#pragma unroll
-    for (int j = 0; j < MOTE_MAX_TOPK; ++j)
-      if (j < k) {
-        r.idx[token * k + j] = sel[j];
-        r.w[token * k + j] = float(sp[j] / div) * r.scale;
-      }
-  }
-  return 0ull;
+  float div = 1.0f;
+  if (r.renorm) div = fmaxf(warp_sum((slot0 < k ? p0 : 0.0f) + (slot1 < k ? p1 : 0.0f)), 1e-20f);
+  if (slot0 < k) { r.idx[token * k + slot0] = lane; r.w[token * k + slot0] = p0 / div * r.scale; }
+  if (slot1 < k) { r.idx[token * k + slot1] = lane + 32; r.w[token * k + slot1] = p1 / div * r.scale; }
 }
 
 // One logit in 64 bits (a warp).
+__device__ __forceinline__ void load8_router(const ScoredRouter& r, int e, int v, float (&w)[8]) {
+  if (r.w_f32) {
+    const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(r.Wr) + int64_t(e) * r.d) + 2 * v;
+    const float4 a = p[0], b = p[1];
+    w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w; w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
+  } else {
+    const uint4 q = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(r.Wr) + int64_t(e) * r.d)[v];
+    w[0] = bf16_lo(q.x); w[1] = bf16_hi(q.x); w[2] = bf16_lo(q.y); w[3] = bf16_hi(q.y);
+    w[4] = bf16_lo(q.z); w[5] = bf16_hi(q.z); w[6] = bf16_lo(q.w); w[7] = bf16_hi(q.w);
+  }
+}
 __device__ __forceinline__ double exact_logit(const ScoredRouter& r, int64_t token, int e, int lane) {
   const uint4* x = reinterpret_cast<const uint4*>(r.x + token * r.ldx);
-  double acc = 0.0;
-  for (int v = lane; v < r.d / 8; v += 32) {
-    const uint4 q = x[v];
-    const float xv[8] = {bf16_lo(q.x), bf16_hi(q.x), bf16_lo(q.y), bf16_hi(q.y), bf16_lo(q.z), bf16_hi(q.z), bf16_lo(q.w), bf16_hi(q.w)};
-    float wv[8];
-    if (r.w_f32) {
-      const float4* w = reinterpret_cast<const float4*>(static_cast<const float*>(r.Wr) + int64_t(e) * r.d) + 2 * v;
-      const float4 a = w[0], b = w[1];
-      wv[0] = a.x; wv[1] = a.y; wv[2] = a.z; wv[3] = a.w; wv[4] = b.x; wv[5] = b.y; wv[6] = b.z; wv[7] = b.w;
-    } else {
-      const uint4 w = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(r.Wr) + int64_t(e) * r.d)[v];
-      wv[0] = bf16_lo(w.x); wv[1] = bf16_hi(w.x); wv[2] = bf16_lo(w.y); wv[3] = bf16_hi(w.y);
-      wv[4] = bf16_lo(w.z); wv[5] = bf16_hi(w.z); wv[6] = bf16_lo(w.w); wv[7] = bf16_hi(w.w);
+  const int n_vec = r.d / 8;
+  double acc[4] = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll 1
+  for (int v0 = lane; v0 < n_vec; v0 += 128) {   // four vectors' loads on their way at a time
+    uint4 q[4];
+    float w[4][8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int v = v0 + 32 * i;
+      q[i] = make_uint4(0u, 0u, 0u, 0u);
+      if (v < n_vec) q[i] = x[v];
+      load8_router(r, e, min(v, n_vec - 1), w[i]);
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) acc = fma(double(xv[j]), double(wv[j]), acc);
+    for (int i = 0; i < 4; ++i) {
+      const float xv[8] = {bf16_lo(q[i].x), bf16_hi(q[i].x), bf16_lo(q[i].y), bf16_hi(q[i].y),
+                           bf16_lo(q[i].z), bf16_hi(q[i].z), bf16_lo(q[i].w), bf16_hi(q[i].w)};
+#pragma unroll
+      for (int j = 0; j < 8; ++j) acc[j & 3] = fma(double(xv[j]), double(w[i][j]), acc[j & 3]);
+    }
   }
-  acc = warp_sum_f(acc);
-  return r.logit_bias ? acc + double(r.logit_bias[e]) : acc;
+  const double l = warp_sum_f64((acc[0] + acc[1]) + (acc[2] + acc[3]));
+  return r.logit_bias ? l + double(r.logit_bias[e]) : l;
 }
 
-// Tokens whose choice is left open by the fp32 scores, kept until all tokens of the CTA are through; then its warps share the
-// logits to be evaluated and each token gets its choice in 64 bits.
+// Tokens whose choice is left open by the fp32 scores, kept until all tokens of the CTA are through; then its warps share the logits to be
+// evaluated, and a warp settles each token.
 template <int kTokens>
-struct RouteDoubt {
+struct RouteDoubts {
   int n;
-  int token[kTokens];                            // number within the CTA's tokens
-  uint64_t which[kTokens];
-  double l[kTokens][64];
+  Doubt d[kTokens];
+  float p[kTokens][64];                            // fp32 scores
+  double l[kTokens][64];                           // exact logits of the experts in doubt
 };
 
-// All warps of the CTA; `first` is the token with number 0.
-template <int kTokens>
-__device__ __forceinline__ void settle_doubts(const ScoredRouter& r, int64_t first, RouteDoubt<kTokens>& q, double (*s_c)[64], int warp,
-                                              int n_warps, int lane) {
-  __syncthreads();
-  const int n = q.n;
-  if (n == 0) return;                            // uniform over the CTA
-  int item = 0;
-  for (int i = 0; i < n; ++i)
-    for (uint64_t m = q.which[i]; m; m &= m - 1, ++item)
-      if (item % n_warps == warp) {
-        const int e = __ffsll((long long)m) - 1;
-        const double l = exact_logit(r, first + q.token[i], e, lane);
-        if (lane == 0) q.l[i][e] = l;
+// The whole choice in 64 bits (a warp; lane holds experts lane and lane + 32): slots of the lane's experts, -1 if they are not taken.
+__device__ __noinline__ void choose_exactly(const ScoredRouter& r, double l0, double l1, double* s_c, int lane, int& slot0, int& slot1) {
+  const int E = r.E;
+  const bool v0 = lane < E, v1 = lane + 32 < E;
+  double c0 = l0, c1 = l1;
+  if (r.select_bias || r.n_groups > 1) {
+    if (r.sigmoid) {
+      c0 = 1.0 / (1.0 + exp(-l0));
+      c1 = 1.0 / (1.0 + exp(-l1));
+    } else {
+      double lm = fmax(v0 ? l0 : -INFINITY, v1 ? l1 : -INFINITY);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) lm = fmax(lm, __shfl_xor_sync(0xffffffffu, lm, o));
+      c0 = v0 ? exp(l0 - lm) : 0.0;
+      c1 = v1 ? exp(l1 - lm) : 0.0;
+      const double den = warp_sum_f64(c0 + c1);
+      c0 /= den;
+      c1 /= den;
+    }
+  }
+  if (r.select_bias) {
+    if (v0) c0 += double(r.select_bias[lane]);
+    if (v1) c1 += double(r.select_bias[lane + 32]);
+  }
+  // the entry with the largest key of 64, of equal ones the lower
+  auto argmax = [&](uint64_t k0, uint64_t k1) {
+    const uint64_t key = k0 > k1 ? k0 : k1;
+    const uint32_t hi = __reduce_max_sync(0xffffffffu, (uint32_t)(key >> 32));
+    const uint32_t lo = __reduce_max_sync(0xffffffffu, (uint32_t)(key >> 32) == hi ? (uint32_t)key : 0u);
+    const uint64_t best = uint64_t(hi) << 32 | lo;
+    const unsigned b0 = __ballot_sync(0xffffffffu, k0 == best), b1 = __ballot_sync(0xffffffffu, k1 == best);
+    return b0 ? __ffs(b0) - 1 : 31 + __ffs(b1);
+  };
+  uint64_t k0 = v0 ? order_key(c0) : 0ull, k1 = v1 ? order_key(c1) : 0ull;
+  if (r.n_groups > 1) {
+    const int G = r.n_groups, per = E / G;
+    __syncwarp();
+    s_c[lane] = c0;
+    s_c[lane + 32] = c1;
+    __syncwarp();
+    uint64_t g0 = 0ull, g1 = 0ull;
+#pragma unroll 1
+    for (int g = lane; g < G; g += 32) {
+      double a = s_c[g * per], b = -INFINITY;
+#pragma unroll 1
+      for (int m = 1; m < per; ++m) {
+        const double v = s_c[g * per + m];
+        b = fmax(b, fmin(a, v));
+        a = fmax(a, v);
       }
-  __syncthreads();
-  for (int i = warp; i < n; i += n_warps) {
-    const double l0 = lane < r.E ? q.l[i][lane] : 0.0, l1 = lane + 32 < r.E ? q.l[i][lane + 32] : 0.0;
-    (void)choose_experts<double>(r, first + q.token[i], l0, l1, 0.0f, s_c[warp], lane);
+      (g < 32 ? g0 : g1) = order_key(per > 1 ? a + b : a);
+    }
+    uint64_t eligible = 0ull;
+#pragma unroll 1
+    for (int j = 0; j < r.topk_groups; ++j) {
+      const int g = argmax(g0, g1);
+      if (lane == (g & 31)) { if (g < 32) g0 = 0ull; else g1 = 0ull; }
+      eligible |= ((1ull << per) - 1ull) << (g * per);
+    }
+    if (!((eligible >> lane) & 1ull)) k0 = 0ull;
+    if (!((eligible >> (lane + 32)) & 1ull)) k1 = 0ull;
+  }
+  slot0 = slot1 = -1;
+#pragma unroll 1
+  for (int j = 0; j < r.k; ++j) {
+    const int e = argmax(k0, k1);
+    if (lane == (e & 31)) {
+      if (e < 32) { slot0 = j; k0 = 0ull; } else { slot1 = j; k1 = 0ull; }
+    }
   }
 }
 
-// The fp32 choice of one token, or its entry among those to be settled.
+// One token in doubt (a warp), its logits evaluated.  false: the border between groups falls differently, so all of its logits are needed.
 template <int kTokens>
-__device__ __forceinline__ void choose_or_defer(const ScoredRouter& r, int64_t first, int number, float l0, float l1, float x_norm2,
-                                                RouteDoubt<kTokens>& q, float* s_c, int lane) {
-  const int64_t token = first + number;
-  if (r.logits) {
-    if (lane < r.E) r.logits[token * r.E + lane] = l0;
-    if (lane + 32 < r.E) r.logits[token * r.E + lane + 32] = l1;
+__device__ __forceinline__ bool settle(const ScoredRouter& r, int64_t t0, const RouteDoubts<kTokens>& q, int i, double* s_c, int lane) {
+  const Doubt& d = q.d[i];
+  const int k = r.k;
+  const double l0 = q.l[i][lane], l1 = q.l[i][lane + 32];
+  int slot0 = -1, slot1 = -1;
+  if (d.full) {
+    choose_exactly(r, l0, l1, s_c, lane, slot0, slot1);
+  } else {
+    const bool m0 = (d.settled >> lane) & 1ull, m1 = (d.settled >> (lane + 32)) & 1ull;
+    double c0 = l0, c1 = l1;                       // exact scores of the settled experts (sigmoid), or their logits
+    if (r.select_bias || r.n_groups > 1) {
+#pragma unroll 1
+      for (int h = 0; h < 2; ++h) {
+        if (!(h ? m1 : m0)) continue;
+        const double c = 1.0 / (1.0 + exp(-(h ? l1 : l0))) + (r.select_bias ? double(r.select_bias[lane + 32 * h]) : 0.0);
+        (h ? c1 : c0) = c;
+      }
+    }
+    __syncwarp();
+    if (d.in >= 0) {
+      // the two largest of either group, among the settled ones
+      const int per = r.E / r.n_groups;
+      double a[2] = {-INFINITY, -INFINITY}, b[2] = {-INFINITY, -INFINITY};
+#pragma unroll 1
+      for (uint64_t m = d.settled; m; m &= m - 1) {
+        const int e = __ffsll((long long)m) - 1, g = e / per;
+        const double x = __shfl_sync(0xffffffffu, c0, e & 31), y = __shfl_sync(0xffffffffu, c1, e & 31), c = e < 32 ? x : y;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          if (g == (h ? d.out : d.in)) {
+            b[h] = fmax(b[h], fmin(a[h], c));
+            a[h] = fmax(a[h], c);
+          }
+      }
+      const double in = per > 1 ? a[0] + b[0] : a[0], out = per > 1 ? a[1] + b[1] : a[1];
+      if (!(in > out || (in == out && d.in < d.out))) return false;
+    }
+    // All others are where they belong: the experts in doubt share out the places that experts in doubt have, in their exact order.
+    const bool w0 = (d.which >> lane) & 1ull, w1 = (d.which >> (lane + 32)) & 1ull;
+    const uint64_t k0 = order_key(c0), k1 = order_key(c1);     // an order of all values, NaN too: no two experts get one place
+    int rank0 = 0, rank1 = 0;                      // how many of them come before the lane's
+#pragma unroll 1
+    for (uint64_t m = d.which; m; m &= m - 1) {
+      const int e = __ffsll((long long)m) - 1;
+      const uint64_t a = __shfl_sync(0xffffffffu, k0, e & 31), b = __shfl_sync(0xffffffffu, k1, e & 31), c = e < 32 ? a : b;
+      rank0 += c > k0 || (c == k0 && e < lane) ? 1 : 0;
+      rank1 += c > k1 || (c == k1 && e < lane + 32) ? 1 : 0;
+    }
+    int place = 0;
+#pragma unroll 1
+    for (int j = 0; j < k; ++j) {
+      const int e = (int)((d.chosen >> (6 * j)) & 63ull);
+      if ((d.which >> e) & 1ull) {
+        if (w0 && rank0 == place) slot0 = j;
+        if (w1 && rank1 == place) slot1 = j;
+        ++place;
+      } else {
+        if (e == lane) slot0 = j;
+        if (e == lane + 32) slot1 = j;
+      }
+    }
   }
-  // (the logit bias, and the last rounding)
-  const float l_max = warp_max(fmaxf(fabsf(l0) < INFINITY ? fabsf(l0) : 0.0f, fabsf(l1) < INFINITY ? fabsf(l1) : 0.0f));
-  const float delta = kLogitEps * sqrtf(x_norm2) * *r.w_norm + 1.2e-7f * l_max;
-  const uint64_t doubt = choose_experts<float>(r, token, l0, l1, delta, s_c, lane);
-  if (doubt == 0ull) return;
-  int slot = 0;
-  if (lane == 0) {
-    slot = atomicAdd(&q.n, 1);
-    q.token[slot] = number;
-    q.which[slot] = doubt;
+  const float p0 = q.p[i][lane], p1 = q.p[i][lane + 32];
+  const float sum = warp_sum((slot0 >= 0 ? p0 : 0.0f) + (slot1 >= 0 ? p1 : 0.0f));
+  const float div = r.renorm ? fmaxf(sum, 1e-20f) : 1.0f;
+  const int64_t at = (t0 + d.token) * k;
+  if (slot0 >= 0) { r.idx[at + slot0] = lane; r.w[at + slot0] = p0 / div * r.scale; }
+  if (slot1 >= 0) { r.idx[at + slot1] = lane + 32; r.w[at + slot1] = p1 / div * r.scale; }
+  return true;
+}
+
+__device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr));      // (in order with the barriers, which are volatile too)
+  return v;
+}
+
+// The choices of tokens rank * share + [0, share) of a tile whose sums lie in parts in the shared memory of the cluster's CTAs: `part` rows of
+// `pitch` floats (E and more), and the squared norms `xx`, at the same places in each.  All threads of the CTA, of which warps 0 ..
+// n_warps - 1 choose; s_c: 64 doubles for each of them.
+template <int kTokens>
+__device__ __forceinline__ void choose_share(const ScoredRouter& r, int64_t t0, int rank, int cluster, int share, const float* part, int pitch,
+                                             const float* xx_part, RouteDoubts<kTokens>& q, double (*s_c)[64],
+                                             int warp, int n_warps, int lane) {
+  const int n = (int)min(int64_t(share), max(int64_t(0), r.T - t0 - rank * share));      // tokens of this CTA that are there
+  if (warp < n_warps && warp < n) {
+    LaneBias bias;
+    bias.load(r, lane);
+    const float w_norm = *r.w_norm;
+    const int E = r.E, e0 = min(lane, E - 1), e1 = min(lane + 32, E - 1);
+    float lb0 = 0.0f, lb1 = 0.0f;
+    if (r.logit_bias) { lb0 = r.logit_bias[e0]; lb1 = r.logit_bias[e1]; }
+#pragma unroll 1
+    for (int i = warp; i < n; i += n_warps) {
+      const int number = rank * share + i;
+      const int64_t token = t0 + number;
+      float l0 = 0.0f, l1 = 0.0f, xx = 0.0f;
+      if (cluster > 1) {                           // the parts' sums, rank by rank
+        const uint32_t row = ptx::smem_u32(part + number * pitch), x_at = ptx::smem_u32(xx_part + number);
+#pragma unroll 2
+        for (int c = 0; c < cluster; ++c) {
+          const uint32_t far = ptx::map_to_rank(row, c);
+          l0 += ld_cluster_f32(far + 4 * e0);
+          l1 += ld_cluster_f32(far + 4 * e1);
+          xx += ld_cluster_f32(ptx::map_to_rank(x_at, c));
+        }
+      } else {
+        l0 = part[number * pitch + e0];
+        l1 = part[number * pitch + e1];
+        xx = xx_part[number];
+      }
+      l0 += lb0;
+      l1 += lb1;
+      if (r.logits) {
+        if (lane < E) r.logits[token * E + lane] = l0;
+        if (lane + 32 < E) r.logits[token * E + lane + 32] = l1;
+      }
+      Doubt d;
+      float p0, p1;
+      choose_experts(r, bias, token, l0, l1, kLogitEps * sqrtf(xx) * w_norm + 1.2e-7f * bias.logit_max, reinterpret_cast<float*>(s_c[warp]), d, p0, p1,
+                     lane);
+      if (d.settled) {
+        int at = 0;
+        if (lane == 0) {
+          at = atomicAdd(&q.n, 1);
+          d.token = number;
+          q.d[at] = d;
+        }
+        at = __shfl_sync(0xffffffffu, at, 0);
+        q.p[at][lane] = p0;
+        q.p[at][lane + 32] = p1;
+      }
+    }
   }
-  slot = __shfl_sync(0xffffffffu, slot, 0);
-  if (lane < r.E) q.l[slot][lane] = double(l0);
-  if (lane + 32 < r.E) q.l[slot][lane + 32] = double(l1);
+  if (cluster > 1) ptx::cluster_sync();            // nobody leaves while its sums are being read
+  else __syncthreads();
+  const int doubts = q.n;
+  if (doubts == 0) return;                         // uniform over the CTA
+  // the logits in doubt, a warp each; then the tokens, a warp each.  A second time for tokens that need all their logits after all.
+#pragma unroll 1
+  for (int again = 0; again < 2; ++again) {
+    int item = 0;
+#pragma unroll 1
+    for (int i = 0; i < doubts; ++i) {
+      if (again && q.d[i].full != 2) continue;
+#pragma unroll 1
+      for (uint64_t m = q.d[i].settled; m; m &= m - 1, ++item)
+        if (item % n_warps == warp) {
+          const int e = __ffsll((long long)m) - 1;
+          const double l = exact_logit(r, t0 + q.d[i].token, e, lane);
+          if (lane == 0) q.l[i][e] = l;
+        }
+    }
+    __syncthreads();
+    bool more = false;
+    if (warp < n_warps)
+#pragma unroll 1
+      for (int i = warp; i < doubts; i += n_warps) {
+        if (again && q.d[i].full != 2) continue;
+        if (!settle(r, t0, q, i, s_c[warp], lane)) {
+          more = true;
+          __syncwarp();
+          if (lane == 0) {
+            q.d[i].full = 2;
+            q.d[i].settled = r.E == 64 ? ~0ull : (1ull << r.E) - 1ull;
+          }
+        }
+      }
+    if (!__syncthreads_or(more)) return;
+  }
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -303,12 +536,6 @@ __device__ __forceinline__ void mma_bf16_k16(float (&c)[4], uint32_t a0, uint32_
 // upper halves of two floats -> bf16x2 (first in the low half)
 __device__ __forceinline__ uint32_t upper_halves(float a, float b) { return __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632); }
 
-__device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
-  return v;
-}
-
 constexpr int kScoredWarps = 8;
 constexpr int kScoredTokens = 16;
 
@@ -319,12 +546,11 @@ template <int NE, bool kF32>
 __global__ void __launch_bounds__(kScoredWarps * 32) route_scored_kernel(ScoredRouter r, int cluster) {
   __shared__ union {
     float part[kScoredWarps][NE * 4][32];
-    struct { RouteDoubt<kScoredTokens> doubt; double c64[kScoredWarps][64]; } late;
+    struct { RouteDoubts<kScoredTokens> doubt; double c[kScoredWarps][64]; } late;
   } sh;
   __shared__ float s_logits[kScoredTokens][NE * 8 + 1];
   __shared__ float s_norm[kScoredWarps][kScoredTokens];
   __shared__ float s_xx[kScoredTokens];
-  __shared__ float s_c[kScoredWarps][64];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int rank = cluster > 1 ? (int)ptx::cluster_ctarank() : 0;
   const int64_t t0 = int64_t(blockIdx.x / cluster) * kScoredTokens;
@@ -364,6 +590,8 @@ __global__ void __launch_bounds__(kScoredWarps * 32) route_scored_kernel(ScoredR
 #pragma unroll
         for (int n = 0; n < NE; ++n) {
           const bool row = in && n * 8 + g < E;
+          // an MMA truncates what it adds up: a step's sum starts from zero and joins the others by a rounded addition
+          float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
           if (kF32) {
             float4 w0 = make_float4(0.f, 0.f, 0.f, 0.f), w1 = w0;
             if (row) {
@@ -380,18 +608,20 @@ __global__ void __launch_bounds__(kScoredWarps * 32) route_scored_kernel(ScoredR
               mid[j] = __uint_as_float(__float_as_uint(r1) & 0xFFFF0000u);
               lo[j] = __fsub_rn(r1, mid[j]);
             }
-            mma_bf16_k16(acc[n], ca.x, cb.x, ca.y, cb.y, upper_halves(hi[0], hi[1]), upper_halves(hi[2], hi[3]));
-            mma_bf16_k16(acc[n], ca.z, cb.z, ca.w, cb.w, upper_halves(hi[4], hi[5]), upper_halves(hi[6], hi[7]));
-            mma_bf16_k16(acc[n], ca.x, cb.x, ca.y, cb.y, upper_halves(mid[0], mid[1]), upper_halves(mid[2], mid[3]));
-            mma_bf16_k16(acc[n], ca.z, cb.z, ca.w, cb.w, upper_halves(mid[4], mid[5]), upper_halves(mid[6], mid[7]));
-            mma_bf16_k16(acc[n], ca.x, cb.x, ca.y, cb.y, upper_halves(lo[0], lo[1]), upper_halves(lo[2], lo[3]));
-            mma_bf16_k16(acc[n], ca.z, cb.z, ca.w, cb.w, upper_halves(lo[4], lo[5]), upper_halves(lo[6], lo[7]));
+            mma_bf16_k16(part, ca.x, cb.x, ca.y, cb.y, upper_halves(hi[0], hi[1]), upper_halves(hi[2], hi[3]));
+            mma_bf16_k16(part, ca.z, cb.z, ca.w, cb.w, upper_halves(hi[4], hi[5]), upper_halves(hi[6], hi[7]));
+            mma_bf16_k16(part, ca.x, cb.x, ca.y, cb.y, upper_halves(mid[0], mid[1]), upper_halves(mid[2], mid[3]));
+            mma_bf16_k16(part, ca.z, cb.z, ca.w, cb.w, upper_halves(mid[4], mid[5]), upper_halves(mid[6], mid[7]));
+            mma_bf16_k16(part, ca.x, cb.x, ca.y, cb.y, upper_halves(lo[0], lo[1]), upper_halves(lo[2], lo[3]));
+            mma_bf16_k16(part, ca.z, cb.z, ca.w, cb.w, upper_halves(lo[4], lo[5]), upper_halves(lo[6], lo[7]));
           } else {
             uint4 w = kZero;
             if (row) w = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(r.Wr) + int64_t(n * 8 + g) * d + s * 32 + t * 8);
-            mma_bf16_k16(acc[n], ca.x, cb.x, ca.y, cb.y, w.x, w.y);
-            mma_bf16_k16(acc[n], ca.z, cb.z, ca.w, cb.w, w.z, w.w);
+            mma_bf16_k16(part, ca.x, cb.x, ca.y, cb.y, w.x, w.y);
+            mma_bf16_k16(part, ca.z, cb.z, ca.w, cb.w, w.z, w.w);
           }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[n][i] += part[i];
         }
         const uint32_t wa[4] = {ca.x, ca.y, ca.z, ca.w}, wb[4] = {cb.x, cb.y, cb.z, cb.w};
 #pragma unroll
@@ -430,54 +660,215 @@ __global__ void __launch_bounds__(kScoredWarps * 32) route_scored_kernel(ScoredR
   if (threadIdx.x == 0) sh.late.doubt.n = 0;
   if (cluster > 1) ptx::cluster_sync();
   else __syncthreads();
-  const int share = kScoredTokens / cluster;     // tokens this CTA chooses for
-  for (int i = warp; i < share; i += kScoredWarps) {
-    const int number = rank * share + i;
-    if (t0 + number >= r.T) break;               // whole warp
-    float l0 = 0.0f, l1 = 0.0f, xx = 0.0f;
-    if (cluster > 1) {
-      const uint32_t a0 = ptx::smem_u32(&s_logits[number][lane < NE * 8 ? lane : 0]);
-      const uint32_t a1 = ptx::smem_u32(&s_logits[number][(lane + 32) % (NE * 8)]);
-      const uint32_t ax = ptx::smem_u32(&s_xx[number]);
-      for (int c = 0; c < cluster; ++c) {
-        l0 += ld_cluster_f32(ptx::map_to_rank(a0, c));
-        if (NE > 4) l1 += ld_cluster_f32(ptx::map_to_rank(a1, c));
-        xx += ld_cluster_f32(ptx::map_to_rank(ax, c));
-      }
-    } else {
-      l0 = s_logits[number][lane < NE * 8 ? lane : 0];
-      if (NE > 4) l1 = s_logits[number][(lane + 32) % (NE * 8)];
-      xx = s_xx[number];
-    }
-    if (r.logit_bias) {
-      if (lane < E) l0 += r.logit_bias[lane];
-      if (lane + 32 < E) l1 += r.logit_bias[lane + 32];
-    }
-    choose_or_defer(r, t0, number, l0, l1, xx, sh.late.doubt, s_c[warp], lane);
-  }
-  if (cluster > 1) ptx::cluster_sync();          // nobody leaves while its sums are being read
-  settle_doubts(r, t0, sh.late.doubt, sh.late.c64, warp, kScoredWarps, lane);
+  choose_share(r, t0, rank, cluster, kScoredTokens / cluster, &s_logits[0][0], NE * 8 + 1, s_xx, sh.late.doubt, sh.late.c, warp,
+               kScoredWarps, lane);
 }
 
-// Largest 2-norm of a router row, rounded up.  One CTA; an offline step.
-__global__ void __launch_bounds__(1024) router_pack_kernel(const void* __restrict__ Wr, int w_f32, int E, int d, float* __restrict__ norm) {
-  __shared__ float s_max[32];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  float worst = 0.0f;
-  for (int e = warp; e < E; e += 32) {
-    double ss = 0.0;
-    for (int j = lane; j < d; j += 32) {
-      const float w = w_f32 ? static_cast<const float*>(Wr)[int64_t(e) * d + j]
-                            : __uint_as_float(uint32_t(static_cast<const uint16_t*>(Wr)[int64_t(e) * d + j]) << 16);
-      ss = fma(double(w), double(w), ss);
-    }
-    worst = fmaxf(worst, __double2float_ru(sqrt(warp_sum_f(ss))));
+// ------------------------------------------------------------------------------------------------
+// Logits of long batches: tcgen05.mma kind::f16, a tile of 128 tokens x all experts per cluster of CTAs that share the width.
+//
+// TMA brings 64 elements of the tokens and of the router's rows (its three bf16 terms, or its bf16 rows) to a stage.  A stage's 4 x terms
+// MMAs form a sum of their own in TMEM -- the tensor core truncates what it adds up, so sums are kept short -- and the epilogue warps
+// add it to fp32 sums in registers, rounded to nearest (eight such accumulators, so that neither side waits for the other).  The same
+// warps read the tokens of the stage from shared memory for their norms.  Then as above: sums meet in distributed shared memory,
+// each CTA chooses for its share of the 128 tokens.
+//
+// Warps: 0 TMA producer, 1 MMA issuer, 2 TMEM owner, 4 to 19 epilogue (four per TMEM lane quarter, 16 experts each); all 32 choose.
+// ------------------------------------------------------------------------------------------------
+constexpr int kTileTokens = 128;
+constexpr int kTileWarps = 16, kTileThreads = 1024;
+constexpr int kTileStageA = kTileTokens * 128;
+constexpr int kTilePipe = 4 * (kTileStageA + 3 * 64 * 128);      // 160 KB: four stages with three terms of 64 experts, more with less
+constexpr int kTileMaxStages = 6;
+constexpr int kTileSums = 8;                                      // accumulators in TMEM, 64 columns each
+constexpr int kTilePitch = 65;
+
+struct __align__(8) TileBarriers {
+  uint64_t full[kTileMaxStages], empty[kTileMaxStages], sum_full[kTileSums], sum_empty[kTileSums];
+  uint32_t tmem_base;
+  int abort_flag;
+};
+struct TileLate {                                                 // over the stages, when they are done with
+  RouteDoubts<kTileTokens> doubt;
+  double c[kTileThreads / 32][64];
+};
+static_assert(sizeof(TileLate) <= kTilePipe, "the choices' data fit over the stages");
+constexpr int kTileSmem = 1024 + kTilePipe + kTileTokens * (kTilePitch + 1) * 4 + (int)sizeof(TileBarriers);
+
+__global__ void __launch_bounds__(kTileThreads, 1)
+route_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w, ScoredRouter r, int cluster, int experts,
+                  int terms, int stages, uint32_t* status) {
+  using namespace ptx;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* gen = smem_raw + (base - smem_u32(smem_raw));
+  float* part = reinterpret_cast<float*>(gen + kTilePipe);
+  float* xx = part + kTileTokens * kTilePitch;
+  TileBarriers* bars = reinterpret_cast<TileBarriers*>(xx + kTileTokens);
+  TileLate* late = reinterpret_cast<TileLate*>(gen);
+  volatile int* abort_flag = &bars->abort_flag;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  const int rank = cluster > 1 ? (int)cluster_ctarank() : 0;
+  const int64_t t0 = int64_t(blockIdx.x / cluster) * kTileTokens;
+  const uint32_t stage_bytes = kTileStageA + uint32_t(terms * experts) * 128;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kTileMaxStages; ++s) { mbar_init(smem_u32(&bars->full[s]), 1); mbar_init(smem_u32(&bars->empty[s]), 1 + kTileWarps); }
+    for (int s = 0; s < kTileSums; ++s) { mbar_init(smem_u32(&bars->sum_full[s]), 1); mbar_init(smem_u32(&bars->sum_empty[s]), kTileWarps); }
+    bars->abort_flag = 0;
+    fence_barrier_init();
+    prefetch_tensormap(&tm_x);
+    prefetch_tensormap(&tm_w);
   }
-  if (lane == 0) s_max[warp] = worst;
+  if (warp == 2) {
+    tmem_alloc(smem_u32(&bars->tmem_base), 64 * kTileSums);
+    tmem_relinquish();
+  }
+  tc_fence_before();
   __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = __shfl_sync(0xffffffffu, bars->tmem_base, 0);
+  pdl_wait();
+  const int n_steps = (r.d + 63) / 64, kb = n_steps * rank / cluster, ke = n_steps * (rank + 1) / cluster;
+
   if (warp == 0) {
-    worst = warp_max(s_max[lane]);
-    if (lane == 0) norm[0] = worst;
+    if (lane == 0) {
+      bool ok = true;
+      int s = 0, phase = 0;
+      for (int ks = kb; ok && ks < ke; ++ks) {
+        ok = mbar_wait(smem_u32(&bars->empty[s]), phase ^ 1, abort_flag);
+        if (!ok) break;
+        const uint32_t bar = smem_u32(&bars->full[s]), dst = base + s * stage_bytes;
+        mbar_expect_tx(bar, stage_bytes);
+        tma_load_2d(dst, &tm_x, ks * 64, (int)t0, bar);
+        tma_load_2d(dst + kTileStageA, &tm_w, ks * 64, 0, bar);
+        if (++s == stages) { s = 0; phase ^= 1; }
+      }
+      // the commits of the last steps have arrived at this CTA's barriers before it may leave
+      for (int i = 0; ok && i < stages; ++i) {
+        ok = mbar_wait(smem_u32(&bars->empty[s]), phase ^ 1, abort_flag);
+        if (++s == stages) { s = 0; phase ^= 1; }
+      }
+    }
+  } else if (warp == 1) {
+    const uint32_t idesc = make_idesc(1, 1, 1, kTileTokens, (uint32_t)experts);
+    int s = 0, phase = 0;
+    for (int ks = kb; ks < ke; ++ks) {
+      const int n = ks - kb, a = n % kTileSums;
+      const bool ok = mbar_wait(smem_u32(&bars->sum_empty[a]), ((n / kTileSums) & 1) ^ 1, abort_flag) &&
+                      mbar_wait(smem_u32(&bars->full[s]), phase, abort_flag);
+      if (!__all_sync(0xffffffffu, ok)) break;
+      tc_fence_after();
+      const uint64_t da = smem_desc_sw128(base + s * stage_bytes);
+      if (elect_one()) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          for (int term = 0; term < terms; ++term)
+            mma_f16(tmem + a * 64, da + 2 * j, smem_desc_sw128(base + s * stage_bytes + kTileStageA + term * experts * 128) + 2 * j, idesc,
+                    j + term > 0 ? 1u : 0u);
+        mma_commit(smem_u32(&bars->empty[s]));
+        mma_commit(smem_u32(&bars->sum_full[a]));
+      }
+      __syncwarp();
+      if (++s == stages) { s = 0; phase ^= 1; }
+    }
+  } else if (warp >= 4 && warp < 4 + kTileWarps) {
+    const int ew = warp - 4, q = warp & 3, col = (ew >> 2) * 16;
+    const bool mine = col < experts;               // (the others only read tokens)
+    float sum[16], sq0 = 0.0f, sq1 = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) sum[j] = 0.0f;
+    int s = 0, phase = 0;
+    for (int ks = kb; ks < ke; ++ks) {
+      const int n = ks - kb, a = n % kTileSums;
+      if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->full[s]), phase, abort_flag))) break;
+      // eight lanes read a token's 128 bytes (in any order), the warp four tokens of either half of the tile
+      const uint8_t* rows = gen + s * stage_bytes + (ew * 4 + (lane >> 3)) * 128 + (lane & 7) * 16;
+      const uint4 v0 = *reinterpret_cast<const uint4*>(rows), v1 = *reinterpret_cast<const uint4*>(rows + 64 * 128);
+      const uint32_t w0[4] = {v0.x, v0.y, v0.z, v0.w}, w1[4] = {v1.x, v1.y, v1.z, v1.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        sq0 = fmaf(bf16_lo(w0[j]), bf16_lo(w0[j]), fmaf(bf16_hi(w0[j]), bf16_hi(w0[j]), sq0));
+        sq1 = fmaf(bf16_lo(w1[j]), bf16_lo(w1[j]), fmaf(bf16_hi(w1[j]), bf16_hi(w1[j]), sq1));
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&bars->empty[s]));
+      if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->sum_full[a]), (n / kTileSums) & 1, abort_flag))) break;
+      tc_fence_after();
+      if (mine) {
+        uint32_t v[16];
+        tmem_ld_32x32b_x16(tmem + (uint32_t(q * 32) << 16) + a * 64 + col, v);
+        tmem_wait_ld();
+#pragma unroll
+        for (int j = 0; j < 16; ++j) sum[j] += __uint_as_float(v[j]);
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&bars->sum_empty[a]));
+      if (++s == stages) { s = 0; phase ^= 1; }
+    }
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) {
+      sq0 += __shfl_xor_sync(0xffffffffu, sq0, o);
+      sq1 += __shfl_xor_sync(0xffffffffu, sq1, o);
+    }
+    if ((lane & 7) == 0) {
+      xx[ew * 4 + (lane >> 3)] = sq0;
+      xx[64 + ew * 4 + (lane >> 3)] = sq1;
+    }
+    if (mine)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) part[(q * 32 + lane) * kTilePitch + col + j] = sum[j];
+  }
+  // after a wait that ran out: time for copies and MMAs in flight to land before shared memory is used anew
+  if (*abort_flag) {
+    const uint64_t start = globaltimer_ns();
+    while (globaltimer_ns() - start < 200000ull) __nanosleep(1000);
+  }
+  tc_fence_before();
+  __syncthreads();                                 // all stages are done with
+  if (threadIdx.x == 0) late->doubt.n = 0;
+  if (warp == 2) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 64 * kTileSums);
+  }
+  if (cluster > 1) cluster_sync();
+  else __syncthreads();
+  if (threadIdx.x == 0 && *abort_flag) atomicExch(status, 1u);
+  choose_share(r, t0, rank, cluster, kTileTokens / cluster, part, kTilePitch, xx, late->doubt, late->c, warp, kTileThreads / 32, lane);
+}
+
+// What a router keeps beside its weights: [0] a device status word, [1] the largest 2-norm of a row (rounded up), and from byte 256 on an
+// fp32 router's three bf16 terms, [3][experts rounded up to 16][d], rows past the last zero.
+constexpr int kPackTerms = 256;
+static int tile_experts(int E) { return (E + 15) & ~15; }
+
+// A CTA per (padded) expert; an offline step.
+__global__ void __launch_bounds__(256) router_pack_kernel(const void* __restrict__ Wr, int w_f32, int E, int d, uint8_t* __restrict__ packed) {
+  __shared__ double s_sum[8];
+  const int e = blockIdx.x, experts = gridDim.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  uint16_t* terms = reinterpret_cast<uint16_t*>(packed + kPackTerms);
+  double ss = 0.0;
+  for (int j = threadIdx.x; j < d; j += 256) {
+    float w = 0.0f;
+    if (e < E)
+      w = w_f32 ? static_cast<const float*>(Wr)[int64_t(e) * d + j]
+                : __uint_as_float(uint32_t(static_cast<const uint16_t*>(Wr)[int64_t(e) * d + j]) << 16);
+    ss = fma(double(w), double(w), ss);
+    if (w_f32) {
+#pragma unroll
+      for (int t = 0; t < 3; ++t) {
+        const uint32_t top = __float_as_uint(w) & 0xFFFF0000u;
+        terms[(int64_t(t) * experts + e) * d + j] = (uint16_t)(top >> 16);
+        w = __fsub_rn(w, __uint_as_float(top));
+      }
+    }
+  }
+  ss = warp_sum_f64(ss);
+  if (lane == 0) s_sum[warp] = ss;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < 8; ++i) ss += s_sum[i];
+    atomicMax(reinterpret_cast<int*>(packed) + 1, __float_as_int(__double2float_ru(sqrt(ss))));      // of non-negative floats
   }
 }
 
@@ -518,21 +909,53 @@ static cudaError_t launch_scored(const ScoredRouter& r, unsigned tiles, int clus
                  : launch_ex(route_scored_kernel<NE, false>, dim3(tiles * cluster), dim3(kScoredWarps * 32), 0, stream, true, cluster, r, cluster);
 }
 
+static cudaError_t launch_tiles(const ScoredRouter& r, const CUtensorMap& tx, const CUtensorMap& tw, int experts, int terms, uint32_t* status,
+                                cudaStream_t stream) {
+  static PerDeviceOnce once;
+  const cudaError_t e = set_max_dynamic_smem(once, route_tile_kernel, kTileSmem);
+  if (e != cudaSuccess) return e;
+  // CTAs that share a tile's width: as many as run at a time, each with two steps at least
+  static ResidentClusters resident;
+  const int64_t tiles = (r.T + kTileTokens - 1) / kTileTokens;
+  int cluster = 1;
+  for (int c = 2; c <= 8; c *= 2)
+    if (tiles <= resident.get(route_tile_kernel, kTileThreads, kTileSmem, c) && r.d >= 128 * c) cluster = c;
+  const int stages = std::min(kTileMaxStages, kTilePipe / (kTileStageA + terms * experts * 128));
+  return launch_ex(route_tile_kernel, dim3((unsigned)(tiles * cluster)), dim3(kTileThreads), kTileSmem, stream, true, cluster, tx, tw, r, cluster,
+                   experts, terms, stages, status);
+}
+
+// From this many tokens on the logits come from the tcgen05 kernel.
+constexpr int64_t kTileMinTokens = 512;
+
+// status: the device status word that a bounded wait raises; null: the router's own
 mote_status_t launch_route_scored(const mote_router_t* R, const void* x, int64_t ldx, int64_t T, int32_t* idx, float* w, float* logits,
-                                  cudaStream_t stream) {
+                                  uint32_t* status, cudaStream_t stream) {
   ScoredRouter r{};
   r.x = static_cast<const uint16_t*>(x); r.ldx = ldx; r.Wr = R->Wr; r.logit_bias = R->logit_bias; r.select_bias = R->select_bias;
-  r.w_norm = static_cast<const float*>(R->packed);
+  r.w_norm = static_cast<const float*>(R->packed) + 1;
   r.T = T; r.d = R->d; r.E = R->E; r.k = R->k; r.sigmoid = R->scoring == MOTE_SCORE_SIGMOID; r.n_groups = R->n_groups;
   r.topk_groups = R->topk_groups; r.renorm = R->renorm != 0; r.w_f32 = R->w_dtype == MOTE_DTYPE_F32; r.scale = R->scale;
   r.idx = idx; r.w = w; r.logits = logits;
-  const unsigned tiles = (unsigned)((T + kScoredTokens - 1) / kScoredTokens);
-  int cluster = 1;                               // CTAs that share a tile's width: as many as the SMs allow
-  while (cluster < 8 && int64_t(tiles) * cluster * 2 <= device_sm_count()) cluster *= 2;
+  if (!status) status = static_cast<uint32_t*>(const_cast<void*>(R->packed));
   const int ne = (R->E + 7) / 8;
-  MOTE_CUDA_OK(ne <= 1   ? launch_scored<1>(r, tiles, cluster, stream)
-               : ne <= 2 ? launch_scored<2>(r, tiles, cluster, stream)
-               : ne <= 4 ? launch_scored<4>(r, tiles, cluster, stream) : launch_scored<8>(r, tiles, cluster, stream));
+  cudaError_t e;
+  if (T >= kTileMinTokens) {
+    const int experts = tile_experts(R->E), terms = r.w_f32 ? 3 : 1;
+    const void* rows = r.w_f32 ? static_cast<const uint8_t*>(R->packed) + kPackTerms : static_cast<const uint8_t*>(R->Wr);
+    CUtensorMap tx, tw;
+    if (!make_operand_map(&tx, x, T, R->d, ldx, kTileTokens) || !make_operand_map(&tw, rows, r.w_f32 ? 3 * experts : R->E, R->d, R->d, terms * experts))
+      return MOTE_ERR_CUDA;
+    e = launch_tiles(r, tx, tw, experts, terms, status, stream);
+  } else {
+    const unsigned tiles = (unsigned)((T + kScoredTokens - 1) / kScoredTokens);
+    int cluster = 1;                             // CTAs that share a tile's width: as many as the SMs allow
+    while (cluster < 8 && int64_t(tiles) * cluster * 2 <= device_sm_count()) cluster *= 2;
+    e = ne <= 1   ? launch_scored<1>(r, tiles, cluster, stream)
+        : ne <= 2 ? launch_scored<2>(r, tiles, cluster, stream)
+        : ne <= 4 ? launch_scored<4>(r, tiles, cluster, stream) : launch_scored<8>(r, tiles, cluster, stream);
+  }
+  if (e != cudaSuccess) return MOTE_ERR_CUDA;
   ++g_launch_count;
   MOTE_LAUNCH_OK();
   return MOTE_OK;
@@ -553,7 +976,7 @@ mote_status_t check_router(const mote_router_t* R) {
 extern "C" size_t mote_router_pack_bytes(int E, int64_t d, int w_dtype) {
   if (E < 1 || E > MOTE_MAX_EXPERTS || d <= 0 || d % 8 != 0 || d > 32768) return 0;
   if (w_dtype != MOTE_DTYPE_F32 && w_dtype != MOTE_DTYPE_BF16) return 0;
-  return 256;
+  return mote::kPackTerms + (w_dtype == MOTE_DTYPE_F32 ? size_t(3) * mote::tile_experts(E) * d * 2 : 0);
 }
 
 extern "C" mote_status_t mote_router_pack(const void* Wr, int w_dtype, int E, int64_t d, void* packed, size_t packed_bytes, void* stream) {
@@ -564,7 +987,9 @@ extern "C" mote_status_t mote_router_pack(const void* Wr, int w_dtype, int E, in
   if (!Wr || !packed) return MOTE_ERR_NULL;
   if (!aligned16(Wr) || (reinterpret_cast<uintptr_t>(packed) & 255u) != 0) return MOTE_ERR_ALIGN;
   if (packed_bytes < need) return MOTE_ERR_WORKSPACE;
-  router_pack_kernel<<<1, 1024, 0, static_cast<cudaStream_t>(stream)>>>(Wr, w_dtype == MOTE_DTYPE_F32, E, (int)d, static_cast<float*>(packed));
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  MOTE_CUDA_OK(cudaMemsetAsync(packed, 0, kPackTerms, s));
+  router_pack_kernel<<<tile_experts(E), 256, 0, s>>>(Wr, w_dtype == MOTE_DTYPE_F32, E, (int)d, static_cast<uint8_t*>(packed));
   MOTE_LAUNCH_OK();
   return MOTE_OK;
 }
@@ -578,5 +1003,5 @@ extern "C" mote_status_t mote_route_scored(const mote_router_t* R, const void* x
   if (T == 0) return MOTE_OK;
   if (!x || !topk_idx || !topk_w) return MOTE_ERR_NULL;
   if (!aligned16(x) || (T > 1 && ldx % 8 != 0)) return MOTE_ERR_ALIGN;
-  return launch_route_scored(R, x, ldx, T, topk_idx, topk_w, logits, static_cast<cudaStream_t>(stream));
+  return launch_route_scored(R, x, T > 1 ? ldx : R->d, T, topk_idx, topk_w, logits, nullptr, static_cast<cudaStream_t>(stream));
 }
