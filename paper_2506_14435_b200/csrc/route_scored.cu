@@ -28,7 +28,7 @@ struct ScoredRouter {
   const float* logit_bias; const float* select_bias;
   const float* w_norm;                  // largest 2-norm of a router row
   int64_t T;
-  int d, E, k, sigmoid, n_groups, topk_groups, renorm, w_f32;
+  int d, E, k, sigmoid, n_groups, per_group, topk_groups, renorm, w_f32;
   float scale;
   int32_t* idx; float* w; float* logits;
 };
@@ -83,9 +83,22 @@ struct Doubt {
   uint64_t chosen;                                 // the fp32 choice, six bits each
 };
 
-// What a lane holds of the router: the biases of its two experts, and their largest magnitudes over all experts.
+// 1 / x and e^x of the special-function unit: a few 2^-23 (and |x| 2^-24) off, which the bounds have room for.
+__device__ __forceinline__ float rcp_approx(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float sqrt_approx(float x) {
+  float y;
+  asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// What a lane holds of the router: the biases and groups of its two experts, and the biases' largest magnitudes over all experts.
 struct LaneBias {
   float s0 = 0.0f, s1 = 0.0f, select_max = 0.0f, logit_max = 0.0f;
+  int group0 = 0, group1 = 0;
   __device__ __forceinline__ void load(const ScoredRouter& r, int lane) {
     const bool v0 = lane < r.E, v1 = lane + 32 < r.E;
     float l0 = 0.0f, l1 = 0.0f;
@@ -98,6 +111,8 @@ struct LaneBias {
       if (v1) l1 = r.logit_bias[lane + 32];
     }
     // (an expert barred by -inf takes no part in the rounding of the others)
+    group0 = lane / r.per_group;
+    group1 = (lane + 32) / r.per_group;
     select_max = warp_max(fmaxf(finite_abs(s0), finite_abs(s1)));
     logit_max = warp_max(fmaxf(finite_abs(l0), finite_abs(l1)));
   }
@@ -114,25 +129,25 @@ __device__ __forceinline__ void choose_experts(const ScoredRouter& r, const Lane
   const bool by_logit = !r.select_bias && r.n_groups == 1;
   float smax = 1.0f;
   if (r.sigmoid) {
-    p0 = 1.0f / (1.0f + expf(-l0));
-    p1 = 1.0f / (1.0f + expf(-l1));
+    p0 = rcp_approx(1.0f + __expf(-l0));
+    p1 = rcp_approx(1.0f + __expf(-l1));
   } else {
     const float lm = warp_max(fmaxf(v0 ? l0 : -INFINITY, v1 ? l1 : -INFINITY));
-    p0 = v0 ? expf(l0 - lm) : 0.0f;
-    p1 = v1 ? expf(l1 - lm) : 0.0f;
-    smax = 1.0f / warp_sum(p0 + p1);
+    p0 = v0 ? __expf(l0 - lm) : 0.0f;
+    p1 = v1 ? __expf(l1 - lm) : 0.0f;
+    smax = rcp_approx(warp_sum(p0 + p1));
     p0 *= smax;
     p1 *= smax;
   }
   const float c0 = (by_logit ? l0 : p0) + bias.s0, c1 = (by_logit ? l1 : p1) + bias.s1;
   // bound on the error of c: of the logit through the score's slope, of expf and the division, of adding the bias
-  const float tau = (by_logit ? delta : r.sigmoid ? 0.25f * delta + 4.8e-7f : smax * (2.0f * delta + 2e-6f)) + 1.2e-7f * bias.select_max;
+  const float tau = (by_logit ? delta : r.sigmoid ? 0.25f * delta + 4.8e-7f : smax * (2.0f * delta + 4e-6f)) + 1.2e-7f * bias.select_max;
   uint32_t k0 = v0 ? order_key(c0) : 0u, k1 = v1 ? order_key(c1) : 0u, best;
   d.full = 0;
   d.which = d.settled = 0ull;
   d.in = d.out = -1;
   if (r.n_groups > 1) {
-    const int G = r.n_groups, per = E / G;
+    const int G = r.n_groups, per = r.per_group;
     __syncwarp();
     s_c[lane] = c0;
     s_c[lane + 32] = c1;
@@ -183,8 +198,8 @@ __device__ __forceinline__ void choose_experts(const ScoredRouter& r, const Lane
         }
       }
     }
-    if (!((kept >> (lane / per)) & 1ull)) k0 = 0u;
-    if (!((kept >> ((lane + 32) / per)) & 1ull)) k1 = 0u;
+    if (!((kept >> bias.group0) & 1ull)) k0 = 0u;
+    if (!((kept >> bias.group1) & 1ull)) k1 = 0u;
   }
   // The k largest.  A lane keeps the place of its experts and the key of the choice before (all choices before an expert's are larger
   // still, so that one is the closest).
@@ -223,13 +238,15 @@ __device__ __forceinline__ void choose_experts(const ScoredRouter& r, const Lane
     d.settled = d.full ? (E == 64 ? ~0ull : (1ull << E) - 1ull) : d.settled | which;
     return;
   }
-  float div = 1.0f;
-  if (r.renorm) div = fmaxf(warp_sum((slot0 < k ? p0 : 0.0f) + (slot1 < k ? p1 : 0.0f)), 1e-20f);
-  if (slot0 < k) { r.idx[token * k + slot0] = lane; r.w[token * k + slot0] = p0 / div * r.scale; }
-  if (slot1 < k) { r.idx[token * k + slot1] = lane + 32; r.w[token * k + slot1] = p1 / div * r.scale; }
+  float mul = r.scale;
+  if (r.renorm) mul *= rcp_approx(fmaxf(warp_sum((slot0 < k ? p0 : 0.0f) + (slot1 < k ? p1 : 0.0f)), 1e-20f));
+  int32_t* idx = r.idx + token * k;
+  float* w = r.w + token * k;
+  if (slot0 < k) { idx[slot0] = lane; w[slot0] = p0 * mul; }
+  if (slot1 < k) { idx[slot1] = lane + 32; w[slot1] = p1 * mul; }
 }
 
-// One logit in 64 bits (a warp).
+// A logit in 64 bits, by four warps a quarter each: its latency is what a long batch waits for.
 __device__ __forceinline__ void load8_router(const ScoredRouter& r, int e, int v, float (&w)[8]) {
   if (r.w_f32) {
     const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(r.Wr) + int64_t(e) * r.d) + 2 * v;
@@ -241,31 +258,30 @@ __device__ __forceinline__ void load8_router(const ScoredRouter& r, int e, int v
     w[4] = bf16_lo(q.z); w[5] = bf16_hi(q.z); w[6] = bf16_lo(q.w); w[7] = bf16_hi(q.w);
   }
 }
-__device__ __forceinline__ double exact_logit(const ScoredRouter& r, int64_t token, int e, int lane) {
+__device__ __forceinline__ double logit_quarter(const ScoredRouter& r, int64_t token, int e, int quarter, int lane) {
   const uint4* x = reinterpret_cast<const uint4*>(r.x + token * r.ldx);
-  const int n_vec = r.d / 8;
+  const int n_vec = r.d / 8, per = (n_vec + 3) / 4, end = min((quarter + 1) * per, n_vec);
   double acc[4] = {0.0, 0.0, 0.0, 0.0};
 #pragma unroll 1
-  for (int v0 = lane; v0 < n_vec; v0 += 128) {   // four vectors' loads on their way at a time
-    uint4 q[4];
-    float w[4][8];
+  for (int v0 = quarter * per + lane; v0 < end; v0 += 64) {      // two vectors' loads on their way at a time
+    uint4 q[2];
+    float w[2][8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 2; ++i) {
       const int v = v0 + 32 * i;
       q[i] = make_uint4(0u, 0u, 0u, 0u);
-      if (v < n_vec) q[i] = x[v];
+      if (v < end) q[i] = x[v];
       load8_router(r, e, min(v, n_vec - 1), w[i]);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 2; ++i) {
       const float xv[8] = {bf16_lo(q[i].x), bf16_hi(q[i].x), bf16_lo(q[i].y), bf16_hi(q[i].y),
                            bf16_lo(q[i].z), bf16_hi(q[i].z), bf16_lo(q[i].w), bf16_hi(q[i].w)};
 #pragma unroll
       for (int j = 0; j < 8; ++j) acc[j & 3] = fma(double(xv[j]), double(w[i][j]), acc[j & 3]);
     }
   }
-  const double l = warp_sum_f64((acc[0] + acc[1]) + (acc[2] + acc[3]));
-  return r.logit_bias ? l + double(r.logit_bias[e]) : l;
+  return warp_sum_f64((acc[0] + acc[1]) + (acc[2] + acc[3]));
 }
 
 // Tokens whose choice is left open by the fp32 scores, kept until all tokens of the CTA are through; then its warps share the logits to be
@@ -276,6 +292,7 @@ struct RouteDoubts {
   Doubt d[kTokens];
   float p[kTokens][64];                            // fp32 scores
   double l[kTokens][64];                           // exact logits of the experts in doubt
+  double quarter[32];                              // a quarter of a sum from each warp
 };
 
 // The whole choice in 64 bits (a warp; lane holds experts lane and lane + 32): slots of the lane's experts, -1 if they are not taken.
@@ -313,7 +330,7 @@ __device__ __noinline__ void choose_exactly(const ScoredRouter& r, double l0, do
   };
   uint64_t k0 = v0 ? order_key(c0) : 0ull, k1 = v1 ? order_key(c1) : 0ull;
   if (r.n_groups > 1) {
-    const int G = r.n_groups, per = E / G;
+    const int G = r.n_groups, per = r.per_group;
     __syncwarp();
     s_c[lane] = c0;
     s_c[lane + 32] = c1;
@@ -373,7 +390,7 @@ __device__ __forceinline__ bool settle(const ScoredRouter& r, int64_t t0, const 
     __syncwarp();
     if (d.in >= 0) {
       // the two largest of either group, among the settled ones
-      const int per = r.E / r.n_groups;
+      const int per = r.per_group;
       double a[2] = {-INFINITY, -INFINITY}, b[2] = {-INFINITY, -INFINITY};
 #pragma unroll 1
       for (uint64_t m = d.settled; m; m &= m - 1) {
@@ -471,7 +488,7 @@ __device__ __forceinline__ void choose_share(const ScoredRouter& r, int64_t t0, 
       }
       Doubt d;
       float p0, p1;
-      choose_experts(r, bias, token, l0, l1, kLogitEps * sqrtf(xx) * w_norm + 1.2e-7f * bias.logit_max, reinterpret_cast<float*>(s_c[warp]), d, p0, p1,
+      choose_experts(r, bias, token, l0, l1, kLogitEps * sqrt_approx(xx) * w_norm + 1.2e-7f * bias.logit_max, reinterpret_cast<float*>(s_c[warp]), d, p0, p1,
                      lane);
       if (d.settled) {
         int at = 0;
@@ -499,10 +516,14 @@ __device__ __forceinline__ void choose_share(const ScoredRouter& r, int64_t t0, 
       if (again && q.d[i].full != 2) continue;
 #pragma unroll 1
       for (uint64_t m = q.d[i].settled; m; m &= m - 1, ++item)
-        if (item % n_warps == warp) {
+        if (warp < n_warps && item % (n_warps / 4) == warp / 4) {
           const int e = __ffsll((long long)m) - 1;
-          const double l = exact_logit(r, t0 + q.d[i].token, e, lane);
-          if (lane == 0) q.l[i][e] = l;
+          const double part = logit_quarter(r, t0 + q.d[i].token, e, warp & 3, lane);
+          if (lane == 0) q.quarter[warp] = part;
+          asm volatile("bar.sync %0, 128;" ::"r"(1 + warp / 4) : "memory");           // the four warps
+          if (lane == 0 && (warp & 3) == 0)
+            q.l[i][e] = ((q.quarter[warp] + q.quarter[warp + 1]) + (q.quarter[warp + 2] + q.quarter[warp + 3])) + (r.logit_bias ? double(r.logit_bias[e]) : 0.0);
+          asm volatile("bar.sync %0, 128;" ::"r"(1 + warp / 4) : "memory");
         }
     }
     __syncthreads();
@@ -669,14 +690,15 @@ __global__ void __launch_bounds__(kScoredWarps * 32) route_scored_kernel(ScoredR
 //
 // TMA brings 64 elements of the tokens and of the router's rows (its three bf16 terms, or its bf16 rows) to a stage.  A stage's 4 x terms
 // MMAs form a sum of their own in TMEM -- the tensor core truncates what it adds up, so sums are kept short -- and the epilogue warps
-// add it to fp32 sums in registers, rounded to nearest (eight such accumulators, so that neither side waits for the other).  The same
-// warps read the tokens of the stage from shared memory for their norms.  Then as above: sums meet in distributed shared memory,
+// add it to fp32 sums in registers, rounded to nearest (eight such accumulators, so that neither side waits for the other).  Eight
+// more warps read the tokens of the stage from shared memory for their norms.  Then as above: sums meet in distributed shared memory,
 // each CTA chooses for its share of the 128 tokens.
 //
-// Warps: 0 TMA producer, 1 MMA issuer, 2 TMEM owner, 4 to 19 epilogue (four per TMEM lane quarter, 16 experts each); all 32 choose.
+// Warps: 0 TMA producer, 1 MMA issuer, 2 TMEM owner, 4 to 19 epilogue (four per TMEM lane quarter, 16 experts each), 20 to 27 norms;
+// all 32 choose.
 // ------------------------------------------------------------------------------------------------
 constexpr int kTileTokens = 128;
-constexpr int kTileWarps = 16, kTileThreads = 1024;
+constexpr int kTileWarps = 16, kTileNormWarps = 8, kTileThreads = 1024;
 constexpr int kTileStageA = kTileTokens * 128;
 constexpr int kTilePipe = 4 * (kTileStageA + 3 * 64 * 128);      // 160 KB: four stages with three terms of 64 experts, more with less
 constexpr int kTileMaxStages = 6;
@@ -712,7 +734,7 @@ route_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constan
   const int64_t t0 = int64_t(blockIdx.x / cluster) * kTileTokens;
   const uint32_t stage_bytes = kTileStageA + uint32_t(terms * experts) * 128;
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kTileMaxStages; ++s) { mbar_init(smem_u32(&bars->full[s]), 1); mbar_init(smem_u32(&bars->empty[s]), 1 + kTileWarps); }
+    for (int s = 0; s < kTileMaxStages; ++s) { mbar_init(smem_u32(&bars->full[s]), 1); mbar_init(smem_u32(&bars->empty[s]), 1 + kTileNormWarps); }
     for (int s = 0; s < kTileSums; ++s) { mbar_init(smem_u32(&bars->sum_full[s]), 1); mbar_init(smem_u32(&bars->sum_empty[s]), kTileWarps); }
     bars->abort_flag = 0;
     fence_barrier_init();
@@ -772,26 +794,13 @@ route_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constan
       if (++s == stages) { s = 0; phase ^= 1; }
     }
   } else if (warp >= 4 && warp < 4 + kTileWarps) {
-    const int ew = warp - 4, q = warp & 3, col = (ew >> 2) * 16;
-    const bool mine = col < experts;               // (the others only read tokens)
-    float sum[16], sq0 = 0.0f, sq1 = 0.0f;
+    const int q = warp & 3, col = ((warp - 4) >> 2) * 16;
+    const bool mine = col < experts;
+    float sum[16];
 #pragma unroll
     for (int j = 0; j < 16; ++j) sum[j] = 0.0f;
-    int s = 0, phase = 0;
-    for (int ks = kb; ks < ke; ++ks) {
-      const int n = ks - kb, a = n % kTileSums;
-      if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->full[s]), phase, abort_flag))) break;
-      // eight lanes read a token's 128 bytes (in any order), the warp four tokens of either half of the tile
-      const uint8_t* rows = gen + s * stage_bytes + (ew * 4 + (lane >> 3)) * 128 + (lane & 7) * 16;
-      const uint4 v0 = *reinterpret_cast<const uint4*>(rows), v1 = *reinterpret_cast<const uint4*>(rows + 64 * 128);
-      const uint32_t w0[4] = {v0.x, v0.y, v0.z, v0.w}, w1[4] = {v1.x, v1.y, v1.z, v1.w};
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        sq0 = fmaf(bf16_lo(w0[j]), bf16_lo(w0[j]), fmaf(bf16_hi(w0[j]), bf16_hi(w0[j]), sq0));
-        sq1 = fmaf(bf16_lo(w1[j]), bf16_lo(w1[j]), fmaf(bf16_hi(w1[j]), bf16_hi(w1[j]), sq1));
-      }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&bars->empty[s]));
+    for (int n = 0; n < ke - kb; ++n) {
+      const int a = n % kTileSums;
       if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->sum_full[a]), (n / kTileSums) & 1, abort_flag))) break;
       tc_fence_after();
       if (mine) {
@@ -804,20 +813,37 @@ route_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constan
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&bars->sum_empty[a]));
-      if (++s == stages) { s = 0; phase ^= 1; }
-    }
-#pragma unroll
-    for (int o = 1; o < 8; o <<= 1) {
-      sq0 += __shfl_xor_sync(0xffffffffu, sq0, o);
-      sq1 += __shfl_xor_sync(0xffffffffu, sq1, o);
-    }
-    if ((lane & 7) == 0) {
-      xx[ew * 4 + (lane >> 3)] = sq0;
-      xx[64 + ew * 4 + (lane >> 3)] = sq1;
     }
     if (mine)
 #pragma unroll
       for (int j = 0; j < 16; ++j) part[(q * 32 + lane) * kTilePitch + col + j] = sum[j];
+  } else if (warp >= 4 + kTileWarps && warp < 4 + kTileWarps + kTileNormWarps) {
+    // eight lanes read a token's 128 bytes (in any order), the warp four tokens of each quarter of the tile
+    const int first = (warp - 4 - kTileWarps) * 4 + (lane >> 3);
+    float sq[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    int s = 0, phase = 0;
+    for (int ks = kb; ks < ke; ++ks) {
+      if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->full[s]), phase, abort_flag))) break;
+      const uint8_t* rows = gen + s * stage_bytes + first * 128 + (lane & 7) * 16;
+      uint4 v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const uint4*>(rows + i * 32 * 128);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sq[i] = fmaf(bf16_lo(w[j]), bf16_lo(w[j]), fmaf(bf16_hi(w[j]), bf16_hi(w[j]), sq[i]));
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&bars->empty[s]));
+      if (++s == stages) { s = 0; phase ^= 1; }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+#pragma unroll
+      for (int o = 1; o < 8; o <<= 1) sq[i] += __shfl_xor_sync(0xffffffffu, sq[i], o);
+      if ((lane & 7) == 0) xx[first + 32 * i] = sq[i];
+    }
   }
   // after a wait that ran out: time for copies and MMAs in flight to land before shared memory is used anew
   if (*abort_flag) {
@@ -935,7 +961,7 @@ mote_status_t launch_route_scored(const mote_router_t* R, const void* x, int64_t
   r.x = static_cast<const uint16_t*>(x); r.ldx = ldx; r.Wr = R->Wr; r.logit_bias = R->logit_bias; r.select_bias = R->select_bias;
   r.w_norm = static_cast<const float*>(R->packed) + 1;
   r.T = T; r.d = R->d; r.E = R->E; r.k = R->k; r.sigmoid = R->scoring == MOTE_SCORE_SIGMOID; r.n_groups = R->n_groups;
-  r.topk_groups = R->topk_groups; r.renorm = R->renorm != 0; r.w_f32 = R->w_dtype == MOTE_DTYPE_F32; r.scale = R->scale;
+  r.per_group = R->E / R->n_groups; r.topk_groups = R->topk_groups; r.renorm = R->renorm != 0; r.w_f32 = R->w_dtype == MOTE_DTYPE_F32; r.scale = R->scale;
   r.idx = idx; r.w = w; r.logits = logits;
   if (!status) status = static_cast<uint32_t*>(const_cast<void*>(R->packed));
   const int ne = (R->E + 7) / 8;
