@@ -6,7 +6,7 @@
 //
 // The choice is the one of exact arithmetic, whatever the order of the sums: scores are computed in fp32 with a bound on
 // their error, and a token whose choice lies within the bound has the scores concerned evaluated once more in 64 bits
-// (a few tokens in a thousand; see RouteDoubt).  So all paths, batch sizes and splits give the same experts.
+// (a few tokens in a thousand; see Doubt).  So all paths, batch sizes and splits give the same experts.
 //
 // Logits: one cluster of CTAs per 16 tokens.  Each warp takes a part of the width and multiplies 16 tokens by all experts with
 // warp-level bf16 MMAs; an fp32 router weight is split exactly into three bf16 terms (8 + 8 + 8 significand bits), so every
@@ -79,7 +79,7 @@ struct Doubt {
   int full;                                        // 1: all logits and the whole choice anew
   int in, out;                                     // the groups on either side of the border, if they are too close; else -1
   uint64_t which;                                  // experts whose order is open
-  uint64_t settled;                                // experts whose logits are evaluated in 64 bits: those, and the groups' (0: no doubt)
+  uint64_t settled;                                // experts whose logits are evaluated in 64 bits: those, and the groups'
   uint64_t chosen;                                 // the fp32 choice, six bits each
 };
 
@@ -119,7 +119,7 @@ struct LaneBias {
 };
 
 // Chooses for one token (a warp) from its logits l0, l1 (off by up to `delta`) and, unless a comparison lies within the error bound, writes
-// the choice.  s_c: 64 floats of the warp's own.  Returned: in `d` what is in doubt (which = 0: nothing, the choice stands), and the
+// the choice.  s_c: 64 floats of the warp's own.  Returned: in `d` what is in doubt (settled = 0: nothing, the choice stands), and the
 // scores of the lane's experts.
 __device__ __forceinline__ void choose_experts(const ScoredRouter& r, const LaneBias& bias, int64_t token, float l0, float l1, float delta,
                                                float* s_c, Doubt& d, float& p0, float& p1, int lane) {
@@ -491,13 +491,19 @@ __device__ __forceinline__ void choose_share(const ScoredRouter& r, int64_t t0, 
       choose_experts(r, bias, token, l0, l1, kLogitEps * sqrt_approx(xx) * w_norm + 1.2e-7f * bias.logit_max, reinterpret_cast<float*>(s_c[warp]), d, p0, p1,
                      lane);
       if (d.settled) {
+        const bool zeros = xx == 0.0f;             // a token of zeros: its logits are the biases, there is nothing to evaluate
         int at = 0;
         if (lane == 0) {
           at = atomicAdd(&q.n, 1);
           d.token = number;
+          if (zeros) { d.full = 1; d.settled = 0ull; }
           q.d[at] = d;
         }
         at = __shfl_sync(0xffffffffu, at, 0);
+        if (zeros) {
+          q.l[at][lane] = double(lb0);
+          q.l[at][lane + 32] = double(lb1);
+        }
         q.p[at][lane] = p0;
         q.p[at][lane + 32] = p1;
       }
@@ -554,6 +560,8 @@ __device__ __forceinline__ void mma_bf16_k16(float (&c)[4], uint32_t a0, uint32_
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// A sum of squares is 0 for zeros only (a token of zeros, as padding is, has logits that are known exactly).
+__device__ __forceinline__ float nonzero_square(float sum, uint32_t bits) { return sum == 0.0f && (bits & 0x7FFF7FFFu) ? 1e-38f : sum; }
 // upper halves of two floats -> bf16x2 (first in the low half)
 __device__ __forceinline__ uint32_t upper_halves(float a, float b) { return __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632); }
 
@@ -586,6 +594,7 @@ __global__ void __launch_bounds__(kScoredWarps * 32) route_scored_kernel(ScoredR
 #pragma unroll
   for (int n = 0; n < NE; ++n) acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.0f;
   float xxa = 0.0f, xxb = 0.0f;
+  uint32_t bits_a = 0u, bits_b = 0u;
   const uint4 kZero = make_uint4(0u, 0u, 0u, 0u);
   pdl_wait();
   constexpr int kAhead = 2;
@@ -647,12 +656,16 @@ __global__ void __launch_bounds__(kScoredWarps * 32) route_scored_kernel(ScoredR
         const uint32_t wa[4] = {ca.x, ca.y, ca.z, ca.w}, wb[4] = {cb.x, cb.y, cb.z, cb.w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
+          bits_a |= wa[j];
+          bits_b |= wb[j];
           xxa = fmaf(bf16_lo(wa[j]), bf16_lo(wa[j]), fmaf(bf16_hi(wa[j]), bf16_hi(wa[j]), xxa));
           xxb = fmaf(bf16_lo(wb[j]), bf16_lo(wb[j]), fmaf(bf16_hi(wb[j]), bf16_hi(wb[j]), xxb));
         }
       }
     }
   }
+  xxa = nonzero_square(xxa, bits_a);
+  xxb = nonzero_square(xxb, bits_b);
 #pragma unroll
   for (int o = 1; o < 4; o <<= 1) {
     xxa += __shfl_xor_sync(0xffffffffu, xxa, o);
@@ -821,6 +834,7 @@ route_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constan
     // eight lanes read a token's 128 bytes (in any order), the warp four tokens of each quarter of the tile
     const int first = (warp - 4 - kTileWarps) * 4 + (lane >> 3);
     float sq[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    uint32_t bits[4] = {0u, 0u, 0u, 0u};
     int s = 0, phase = 0;
     for (int ks = kb; ks < ke; ++ks) {
       if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->full[s]), phase, abort_flag))) break;
@@ -831,6 +845,7 @@ route_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constan
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+        bits[i] |= w[0] | w[1] | w[2] | w[3];
 #pragma unroll
         for (int j = 0; j < 4; ++j) sq[i] = fmaf(bf16_lo(w[j]), bf16_lo(w[j]), fmaf(bf16_hi(w[j]), bf16_hi(w[j]), sq[i]));
       }
@@ -840,6 +855,7 @@ route_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constan
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
+      sq[i] = nonzero_square(sq[i], bits[i]);
 #pragma unroll
       for (int o = 1; o < 8; o <<= 1) sq[i] += __shfl_xor_sync(0xffffffffu, sq[i], o);
       if ((lane & 7) == 0) xx[first + 32 * i] = sq[i];
@@ -951,8 +967,11 @@ static cudaError_t launch_tiles(const ScoredRouter& r, const CUtensorMap& tx, co
                    experts, terms, stages, status);
 }
 
-// From this many tokens on the logits come from the tcgen05 kernel.
-constexpr int64_t kTileMinTokens = 512;
+// The logits come from the tcgen05 kernel from this many column tiles of 8 experts on, counted for every token and every bf16 term of the
+// weights.  us, warp-level MMAs / tcgen05: 64 experts in fp32, d = 2048: 14 / 17 at 512 tokens, 20 / 16.5 at 768, 34 / 20 at 2048, 75 / 30
+// at 8192; 16 experts in fp32: 11 / 14 at 2048, 14 / 16 at 4096, 29 / 22 at 8192; 60 in bf16, d = 896: 9.9 / 13.5 at 1024, 14.4 / 12.9 at
+// 2048; 8 in bf16, d = 1536: 12.5 / 17.5 at 8192.
+constexpr int64_t kTileMinWork = 16384;
 
 // status: the device status word that a bounded wait raises; null: the router's own
 mote_status_t launch_route_scored(const mote_router_t* R, const void* x, int64_t ldx, int64_t T, int32_t* idx, float* w, float* logits,
@@ -966,7 +985,7 @@ mote_status_t launch_route_scored(const mote_router_t* R, const void* x, int64_t
   if (!status) status = static_cast<uint32_t*>(const_cast<void*>(R->packed));
   const int ne = (R->E + 7) / 8;
   cudaError_t e;
-  if (T >= kTileMinTokens) {
+  if (T * ne * (r.w_f32 ? 3 : 1) >= kTileMinWork) {
     const int experts = tile_experts(R->E), terms = r.w_f32 ? 3 : 1;
     const void* rows = r.w_f32 ? static_cast<const uint8_t*>(R->packed) + kPackTerms : static_cast<const uint8_t*>(R->Wr);
     CUtensorMap tx, tw;

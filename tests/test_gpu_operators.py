@@ -143,6 +143,19 @@ def test_route_scored_takes_any_values_without_leaving_the_experts(mote, T):
             assert int(s.min()) >= 0 and int(s.max()) < 16 and bool((s[:, 1:] > s[:, :-1]).all())
 
 
+@pytest.mark.parametrize("T", [3, 40, 2100])
+@pytest.mark.parametrize("scoring,n_groups,lb,sb", [("softmax", 1, False, False), ("sigmoid", 8, False, True), ("sigmoid", 8, True, False), ("softmax", 4, True, True)])
+def test_route_scored_padded_batches_and_tiny_tokens(mote, T, scoring, n_groups, lb, sb):
+    """Tokens of zeros have the biases for logits; tokens whose squares underflow are still told apart exactly."""
+    E, d = 64, 512
+    x = _randn(81, T, d)
+    x[1::3] = 0.0
+    x[2::3] *= 1e-30
+    bias = lambda seed: (_randn(seed, E // 2) * 0.01).repeat_interleave(2).contiguous()
+    check_route(mote, x.bfloat16(), _randn(82, E, d) * 0.02, 6, bias(83) if lb else None, bias(84) if sb else None, scoring=scoring,
+                n_groups=n_groups, topk_groups=max(1, n_groups // 2))
+
+
 def test_route_scored_strided_rows_and_empty_batches(mote):
     wide = _randn(15, 50, 640).bfloat16()
     Wr = _randn(16, 24, 320) * 0.02
