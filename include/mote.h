@@ -196,7 +196,7 @@ mote_status_t mote_route_stats(const float* logits, const int32_t* topk_idx, int
  *   groups   : the experts in n_groups runs of E / n_groups; a group counts the sum of its two largest c (its one c
  *              if it has one expert); the topk_groups largest stay, ties to the lower group
  *   choice   : the k largest c among the experts of those groups, in descending order, ties to the lower expert
- *              index.  Without select_bias and groups the order is that of the logits.
+ *              index.  Without select_bias the order is that of the logits, which scores grow with.
  *   w_j      = scale * s_j / max(sum of the k chosen s, 1e-20) if renorm, else scale * s_j
  *
  * The choice is that of exact arithmetic: where fp32 scores are too close to tell, the logits concerned are evaluated

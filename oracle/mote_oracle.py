@@ -408,8 +408,8 @@ def rms_norm(x_bf16: np.ndarray, eps: float) -> np.ndarray:
 def route_scored(x: np.ndarray, Wr: np.ndarray, k: int, *, scoring="softmax", logit_bias=None, select_bias=None, n_groups=1,
                  topk_groups=1, renorm=True, scale=1.0):
     """Router with softmax or sigmoid scores, a bias that takes part in the choice alone, groups and renormalised weights, fp64,
-    token by token.  x [T, d] and Wr [E, d] as fp64 values of the stored ones.  Without select_bias and groups the experts are
-    ordered by logit (scores grow with it), else by c = score + select_bias; a tie goes to the lower index."""
+    token by token.  x [T, d] and Wr [E, d] as fp64 values of the stored ones.  Without select_bias the experts are ordered
+    by logit (scores grow with it), else by c = score + select_bias; a tie goes to the lower index."""
     T, E = x.shape[0], Wr.shape[0]
     l = x.astype(np.float64) @ Wr.astype(np.float64).T
     if logit_bias is not None:
@@ -423,13 +423,12 @@ def route_scored(x: np.ndarray, Wr: np.ndarray, k: int, *, scoring="softmax", lo
         else:
             with np.errstate(over="ignore"):
                 s = 1.0 / (1.0 + np.exp(-l[t]))
-        c = l[t] if select_bias is None and n_groups == 1 else s
-        if select_bias is not None:
-            c = c + np.asarray(select_bias, np.float64)
+        c = s if select_bias is None else s + np.asarray(select_bias, np.float64)
         group = [sum(sorted(c[g * per:(g + 1) * per], reverse=True)[:2]) for g in range(n_groups)]
         kept = sorted(range(n_groups), key=lambda g: (-group[g], g))[:topk_groups]
         open_ = [e for e in range(E) if e // per in kept]
-        pick = sorted(open_, key=lambda e: (-c[e], e))[:k]
+        order = l[t] if select_bias is None else c
+        pick = sorted(open_, key=lambda e: (-order[e], e))[:k]
         idx[t] = pick
         w[t] = scale * s[pick] / (max(s[pick].sum(), 1e-20) if renorm else 1.0)
     return dict(logits=l, idx=idx, w=w, near_tie=np.zeros(T, dtype=bool))

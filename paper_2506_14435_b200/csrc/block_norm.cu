@@ -5,8 +5,11 @@
 //   n  = bf16( r' * rsqrt(mean(r'^2) + eps) * pre_gain )        norm before the next block, of the stored r'
 //
 // HBM-bound: y and the residual are read once, r' and n written once (8 bytes an element with a bf16 stream, 12 with an
-// fp32 one).  A row stays in the registers of its threads between the passes (y and r as packed vectors of 8 elements);
-// sums are fp32 in a fixed tree, so a row's result depends on its width alone.
+// fp32 one).  A row stays in the registers of its threads between the passes; sums are fp32 in a fixed tree that goes by the row's
+// width alone, so a row's result does not depend on the batch.
+//
+// 8192 x 2048, norms on both sides, bf16 stream: 28 us, 4 800 GB/s (a plain copy of the same bytes 23).  A row per CTA, weights read for
+// each: 42; rows side by side, fp32 instructions one at a time: 36 to 47, at 51 instructions an element.
 #include <algorithm>
 
 #include "mote_common.cuh"
@@ -115,30 +118,33 @@ struct ColumnWeights {
   Eight mix[kHeld ? kVec : 1], pre[kHeld ? kVec : 1];
   int64_t gate_row;                       // the gate row that `mix` holds (-1: none yet)
 };
+__device__ __forceinline__ Eight acted_gate(const BlockNormArgs& a, Eight g) {
+  if (a.gate_sigmoid)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float lo, hi;
+      unpack_f32x2(g.p[j], lo, hi);
+      g.p[j] = f32x2(sigmoid_f32(lo), sigmoid_f32(hi));
+    }
+  return g;
+}
 __device__ __forceinline__ Eight mixed_weights(const BlockNormArgs& a, int64_t gate_row, int col) {
   Eight m;
 #pragma unroll
   for (int j = 0; j < 4; ++j) m.p[j] = f32x2(1.0f, 1.0f);
   if (a.post_gain) m = load8_f32(a.post_gain + col);
-  if (a.gate_cols > 1) {
-    Eight g = a.gate_f32 ? load8_f32(static_cast<const float*>(a.gate) + gate_row * a.d + col)
-                         : unpack8(*reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.gate) + gate_row * a.d + col));
-    if (a.gate_sigmoid)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        float lo, hi;
-        unpack_f32x2(g.p[j], lo, hi);
-        g.p[j] = f32x2(sigmoid_f32(lo), sigmoid_f32(hi));
-      }
-    m = m * g;
-  }
+  if (a.gate_cols > 1)
+    m = m * acted_gate(a, a.gate_f32 ? load8_f32(static_cast<const float*>(a.gate) + gate_row * a.d + col)
+                                     : unpack8(*reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.gate) + gate_row * a.d + col)));
   return m;
 }
 
-// One row.  Threads of a row that is not there (row >= T) go along as zeros.
-template <int kVec, bool kF32>
+// One row.  Threads of a row that is not there (row >= T) go along as zeros.  gv: the row's own gate vectors, kGate (1: bf16, 2: fp32)
+// units of 16 bytes each; kGate = 0: the gate is read here.
+template <int kVec, bool kF32, int kGate>
 __device__ __forceinline__ void norm_row(const BlockNormArgs& a, int64_t row, int group, int sub, int tid, const uint4 (&yv)[kVec],
-                                         Stored8<kF32> (&rv)[kVec], ColumnWeights<kVec>& cw, float* s_post, float* s_pre) {
+                                         Stored8<kF32> (&rv)[kVec], const Stored8<kGate == 2> (&gv)[kVec], ColumnWeights<kVec>& cw, float* s_post,
+                                         float* s_pre) {
   constexpr bool kHeld = ColumnWeights<kVec>::kHeld;
   const bool live = row < a.T;
   float mul = a.scale;
@@ -169,8 +175,13 @@ __device__ __forceinline__ void norm_row(const BlockNormArgs& a, int64_t row, in
     Eight p = unpack8(yv[i]);
     if (weighted) {
       Eight& m = cw.mix[kHeld ? i : 0];
-      if (!kHeld || gate_row != cw.gate_row) m = mixed_weights(a, gate_row, col);
-      p = p * m;
+      if (kGate) {                        // (`mix` holds the gain alone)
+        const Eight g = acted_gate(a, gv[i].get());
+        p = p * (!a.post_gain ? g : (kHeld ? m : load8_f32(a.post_gain + col)) * g);      // (the products of mixed_weights, in its order)
+      } else {
+        if (!kHeld || gate_row != cw.gate_row) m = mixed_weights(a, gate_row, col);
+        p = p * m;
+      }
     }
     Eight x = rv[i].get();
 #pragma unroll
@@ -196,12 +207,16 @@ __device__ __forceinline__ void norm_row(const BlockNormArgs& a, int64_t row, in
     *reinterpret_cast<uint4*>(a.normed_out + out_at + i * group * 8) = pack8(x);
   }
 }
-template <int kVec>
+template <int kVec, int kGate>
 __device__ __forceinline__ void start_weights(const BlockNormArgs& a, int group, int tid, ColumnWeights<kVec>& cw) {
   cw.gate_row = -1;
-  if (ColumnWeights<kVec>::kHeld && a.pre_gain)
+  if (ColumnWeights<kVec>::kHeld)
 #pragma unroll
-    for (int i = 0; i < kVec; ++i) cw.pre[ColumnWeights<kVec>::kHeld ? i : 0] = load8_f32(a.pre_gain + min((i * group + tid) * 8, a.d - 8));
+    for (int i = 0; i < kVec; ++i) {
+      const int col = min((i * group + tid) * 8, a.d - 8);
+      if (a.pre_gain) cw.pre[ColumnWeights<kVec>::kHeld ? i : 0] = load8_f32(a.pre_gain + col);
+      if (kGate && a.post_gain) cw.mix[ColumnWeights<kVec>::kHeld ? i : 0] = load8_f32(a.post_gain + col);
+    }
 }
 
 // A row (or several, of few threads each) per CTA.
@@ -228,8 +243,9 @@ __global__ void __launch_bounds__(512) block_norm_kernel(BlockNormArgs a, int gr
     }
   }
   ColumnWeights<kVec> cw;
-  start_weights(a, group, tid, cw);
-  norm_row<kVec, kF32>(a, row, group, sub, tid, yv, rv, cw, s_post, s_pre);
+  start_weights<kVec, 0>(a, group, tid, cw);
+  const Stored8<false> none[kVec] = {};
+  norm_row<kVec, kF32, 0>(a, row, group, sub, tid, yv, rv, none, cw, s_post, s_pre);
 }
 
 // Many rows: the threads of a row walk over rows.  A thread fetches its own vectors of the rows to come into shared memory
@@ -238,84 +254,107 @@ __global__ void __launch_bounds__(512) block_norm_kernel(BlockNormArgs a, int gr
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
-constexpr int kNormStages = 4;
-template <int kVec, bool kF32>
+// 16-byte units of a thread's vector: y, the stream's one or two, and those of a gate that has a row for each token.  Four rows ahead where two
+// CTAs of them fit an SM.  (8192 x 2048: three stages 32 us, six 29; three CTAs per SM, whose registers spill, 33.)
+template <int kVec, bool kF32, int kGate>
+struct NormRing {
+  static constexpr int kUnits = 1 + (kF32 ? 2 : 1) + kGate;
+  static constexpr int kStages = kVec * kUnits <= 6 ? 4 : kVec * kUnits <= 8 ? 3 : 2;
+  static constexpr int kStageBytes = kVec * kUnits * 16;                   // per thread
+};
+template <int kVec, bool kF32, int kGate>
 __global__ void __launch_bounds__(256, 2) block_norm_stream_kernel(BlockNormArgs a, int group) {
-  constexpr int kUnits = 1 + (kF32 ? 2 : 1);               // 16-byte units of a thread's vector: y, and the stream's one or two
+  using R = NormRing<kVec, kF32, kGate>;
+  constexpr int kUnits = R::kUnits, kStages = R::kStages, kResUnits = kF32 ? 2 : 1;
   extern __shared__ uint4 s_ring[];                        // [stage][vector][unit][thread]
   __shared__ __align__(16) float s_post[2][8], s_pre[2][8];
+  const int threads = blockDim.x, rows = threads / group;
   const int sub = threadIdx.x / group, tid = threadIdx.x - sub * group;
-  const int64_t step = int64_t(gridDim.x) * (256 / group);
+  const int64_t step = int64_t(gridDim.x) * rows;
   const uint32_t ring = (uint32_t)__cvta_generic_to_shared(s_ring) + threadIdx.x * 16;
   auto fetch = [&](int64_t row, int stage) {
     if (row < a.T) {
       const uint16_t* y = a.y + row * a.ldy + tid * 8;
       const char* res = static_cast<const char*>(a.res) + (row * a.ldr + tid * 8) * (kF32 ? 4 : 2);
+      const char* gate = static_cast<const char*>(a.gate) + (row * a.d + tid * 8) * (kGate == 2 ? 4 : 2);
 #pragma unroll
       for (int i = 0; i < kVec; ++i) {
         if ((i * group + tid) * 8 >= a.d) continue;
-        const uint32_t dst = ring + ((stage * kVec + i) * kUnits) * (256 * 16);
+        const uint32_t dst = ring + ((stage * kVec + i) * kUnits) * (threads * 16);
         cp_async16(dst, y + i * group * 8);
         if (a.res)
 #pragma unroll
-          for (int u = 0; u < kUnits - 1; ++u) cp_async16(dst + (1 + u) * (256 * 16), res + i * group * 8 * (kF32 ? 4 : 2) + u * 16);
+          for (int u = 0; u < kResUnits; ++u) cp_async16(dst + (1 + u) * (threads * 16), res + i * group * 8 * (kF32 ? 4 : 2) + u * 16);
+#pragma unroll
+        for (int u = 0; u < kGate; ++u)
+          cp_async16(dst + (1 + kResUnits + u) * (threads * 16), gate + i * group * 8 * (kGate == 2 ? 4 : 2) + u * 16);
       }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
   // what no copy fills (past the row's end, no residual) reads as zeros
 #pragma unroll
-  for (int i = 0; i < kNormStages * kVec * kUnits; ++i) {
-    const bool copied = ((i / kUnits % kVec) * group + tid) * 8 < a.d && (i % kUnits == 0 || a.res);
-    if (!copied) s_ring[i * 256 + threadIdx.x] = make_uint4(0u, 0u, 0u, 0u);
+  for (int i = 0; i < kStages * kVec * kUnits; ++i) {
+    const int unit = i % kUnits;
+    const bool copied = ((i / kUnits % kVec) * group + tid) * 8 < a.d && (unit == 0 || unit > kResUnits || a.res);
+    if (!copied) s_ring[i * threads + threadIdx.x] = make_uint4(0u, 0u, 0u, 0u);
   }
   pdl_wait();
   ColumnWeights<kVec> cw;
-  start_weights(a, group, tid, cw);
-  int64_t row = int64_t(blockIdx.x) * (256 / group) + sub;
+  start_weights<kVec, kGate>(a, group, tid, cw);
+  int64_t row = int64_t(blockIdx.x) * rows + sub;
 #pragma unroll
-  for (int s = 0; s < kNormStages - 1; ++s) fetch(row + s * step, s);
-  int stage = 0, ahead = kNormStages - 1, parity = 0;
+  for (int s = 0; s < kStages - 1; ++s) fetch(row + s * step, s);
+  int stage = 0, ahead = kStages - 1, parity = 0;
   for (; row < a.T; row += step) {                         // all threads of a row together
-    fetch(row + (kNormStages - 1) * step, ahead);
-    asm volatile("cp.async.wait_group %0;" ::"n"(kNormStages - 1) : "memory");
+    fetch(row + (kStages - 1) * step, ahead);
+    asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
     uint4 yv[kVec];
     Stored8<kF32> rv[kVec];
+    Stored8<kGate == 2> gv[kVec];
 #pragma unroll
     for (int i = 0; i < kVec; ++i) {
-      const uint4* from = s_ring + ((stage * kVec + i) * kUnits) * 256 + threadIdx.x;
+      const uint4* from = s_ring + ((stage * kVec + i) * kUnits) * threads + threadIdx.x;
       yv[i] = from[0];
 #pragma unroll
-      for (int u = 0; u < kUnits - 1; ++u) rv[i].v[u] = from[(1 + u) * 256];
+      for (int u = 0; u < kResUnits; ++u) rv[i].v[u] = from[(1 + u) * threads];
+#pragma unroll
+      for (int u = 0; u < kGate; ++u) gv[i].v[u] = from[(1 + kResUnits + u) * threads];
     }
-    norm_row<kVec, kF32>(a, row, group, sub, tid, yv, rv, cw, s_post[parity], s_pre[parity]);
+    norm_row<kVec, kF32, kGate>(a, row, group, sub, tid, yv, rv, gv, cw, s_post[parity], s_pre[parity]);
     ahead = stage;
-    stage = stage + 1 == kNormStages ? 0 : stage + 1;
+    stage = stage + 1 == kStages ? 0 : stage + 1;
     parity ^= 1;
   }
 }
 
 template <int kVec>
 static cudaError_t launch_block_norm(const BlockNormArgs& a, bool res_f32, int group, cudaStream_t stream) {
-  const int threads = std::max(group, 128), rows = threads / group;
+  const int rows = std::max(1, 128 / group), threads = rows * group;
   const unsigned grid = (unsigned)((a.T + rows - 1) / rows);
   return res_f32 ? launch_pdl(block_norm_kernel<kVec, true>, dim3(grid), dim3(threads), 0, stream, a, group)
                  : launch_pdl(block_norm_kernel<kVec, false>, dim3(grid), dim3(threads), 0, stream, a, group);
 }
-template <int kVec, bool kF32>
+template <int kVec, bool kF32, int kGate>
 static cudaError_t launch_stream_as(const BlockNormArgs& a, int group, cudaStream_t stream) {
-  const int smem = kNormStages * kVec * (kF32 ? 3 : 2) * 16 * 256;
+  using R = NormRing<kVec, kF32, kGate>;
   static PerDeviceOnce once;
-  const cudaError_t e = set_max_dynamic_smem(once, block_norm_stream_kernel<kVec, kF32>, smem);
+  const cudaError_t e = set_max_dynamic_smem(once, block_norm_stream_kernel<kVec, kF32, kGate>, R::kStages * R::kStageBytes * 256);
   if (e != cudaSuccess) return e;
-  const int64_t blocks = (a.T + 256 / group - 1) / (256 / group);
-  const int per_sm = std::min(2, 220 * 1024 / (smem + 2048));
-  return launch_pdl(block_norm_stream_kernel<kVec, kF32>, dim3((unsigned)std::min<int64_t>(blocks, device_sm_count() * per_sm)), dim3(256), smem,
-                    stream, a, group);
+  const int rows = std::max(1, 256 / group), threads = rows * group, smem = R::kStages * R::kStageBytes * threads;
+  const int64_t blocks = (a.T + rows - 1) / rows;
+  const int per_sm = std::max(1, std::min(512 / threads, 220 * 1024 / (smem + 2048)));
+  return launch_pdl(block_norm_stream_kernel<kVec, kF32, kGate>, dim3((unsigned)std::min<int64_t>(blocks, device_sm_count() * per_sm)), dim3(threads),
+                    smem, stream, a, group);
+}
+template <int kVec, bool kF32>
+static cudaError_t launch_stream_gate(const BlockNormArgs& a, int group, cudaStream_t stream) {
+  if (a.gate_cols <= 1 || a.gate_tokens != 1) return launch_stream_as<kVec, kF32, 0>(a, group, stream);
+  return a.gate_f32 ? launch_stream_as<kVec, kF32, 2>(a, group, stream) : launch_stream_as<kVec, kF32, 1>(a, group, stream);
 }
 template <int kVec>
 static cudaError_t launch_block_norm_stream(const BlockNormArgs& a, bool res_f32, int group, cudaStream_t stream) {
-  return res_f32 ? launch_stream_as<kVec, true>(a, group, stream) : launch_stream_as<kVec, false>(a, group, stream);
+  return res_f32 ? launch_stream_gate<kVec, true>(a, group, stream) : launch_stream_gate<kVec, false>(a, group, stream);
 }
 
 // [a, a + na) and [b, b + nb) share a byte
@@ -373,9 +412,9 @@ extern "C" mote_status_t mote_block_norm(const mote_block_norm_t* N, const void*
   // Threads of a row, by its width alone, so that a row's sums do not depend on T: two vectors a thread (one in rows of up to 256
   // elements), more where that takes over 256 threads, and up to 512 threads for rows of more than 8192 elements.
   const int most = n_vec <= 1024 ? 256 : 512;
-  int vec = n_vec <= 32 ? 1 : 2, group = 32;
+  int vec = n_vec <= 32 ? 1 : 2;
   while (vec * most < n_vec) vec *= 2;
-  while (group * vec < n_vec) group *= 2;
+  const int group = ((n_vec + vec - 1) / vec + 31) / 32 * 32;
   if (n_vec <= 1024 && T >= int64_t(device_sm_count()) * 8)            // rows enough to walk over
     e = vec == 4   ? launch_block_norm_stream<4>(a, f32, group, s)
         : vec == 2 ? launch_block_norm_stream<2>(a, f32, group, s) : launch_block_norm_stream<1>(a, f32, group, s);

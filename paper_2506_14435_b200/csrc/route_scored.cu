@@ -78,6 +78,7 @@ struct Doubt {
   int token;                                       // number within the CTA's tokens
   int full;                                        // 1: all logits and the whole choice anew
   int in, out;                                     // the groups on either side of the border, if they are too close; else -1
+  float l_max, inv_den, den_rel;                   // softmax: what is taken off the logits, 1 / denominator and the bound on its relative error
   uint64_t which;                                  // experts whose order is open
   uint64_t settled;                                // experts whose logits are evaluated in 64 bits: those, and the groups'
   uint64_t chosen;                                 // the fp32 choice, six bits each
@@ -125,9 +126,11 @@ __device__ __forceinline__ void choose_experts(const ScoredRouter& r, const Lane
                                                float* s_c, Doubt& d, float& p0, float& p1, int lane) {
   const int E = r.E, k = r.k;
   const bool v0 = lane < E, v1 = lane + 32 < E;
-  // Both scores grow with the logit: without a bias and without groups (whose sums need the scores) the logits are compared.
-  const bool by_logit = !r.select_bias && r.n_groups == 1;
+  // Both scores grow with the logit: without a bias logits are compared, except for the groups, whose sums need the scores.  Sums of a
+  // softmax's are then compared relative to their size (the denominator cancels).
+  const bool by_logit = !r.select_bias && r.n_groups == 1, ratios = !r.sigmoid && !r.select_bias;
   float smax = 1.0f;
+  d.l_max = d.inv_den = d.den_rel = 0.0f;
   if (r.sigmoid) {
     p0 = rcp_approx(1.0f + __expf(-l0));
     p1 = rcp_approx(1.0f + __expf(-l1));
@@ -136,12 +139,15 @@ __device__ __forceinline__ void choose_experts(const ScoredRouter& r, const Lane
     p0 = v0 ? __expf(l0 - lm) : 0.0f;
     p1 = v1 ? __expf(l1 - lm) : 0.0f;
     smax = rcp_approx(warp_sum(p0 + p1));
+    d.l_max = lm;
+    d.inv_den = smax;
+    d.den_rel = delta < 1.0f ? delta * (1.0f + delta) + 4e-6f : 1e30f;      // e^delta - 1
     p0 *= smax;
     p1 *= smax;
   }
   const float c0 = (by_logit ? l0 : p0) + bias.s0, c1 = (by_logit ? l1 : p1) + bias.s1;
   // bound on the error of c: of the logit through the score's slope, of expf and the division, of adding the bias
-  const float tau = (by_logit ? delta : r.sigmoid ? 0.25f * delta + 4.8e-7f : smax * (2.0f * delta + 4e-6f)) + 1.2e-7f * bias.select_max;
+  float tau = (by_logit ? delta : r.sigmoid ? 0.25f * delta + 4.8e-7f : delta < 0.5f ? smax * (2.0f * delta * (1.0f + 2.0f * delta) + 4e-6f) : 1e30f) + 1.2e-7f * bias.select_max;
   uint32_t k0 = v0 ? order_key(c0) : 0u, k1 = v1 ? order_key(c1) : 0u, best;
   d.full = 0;
   d.which = d.settled = 0ull;
@@ -179,7 +185,16 @@ __device__ __forceinline__ void choose_experts(const ScoredRouter& r, const Lane
     }
     if (r.topk_groups < G) {
       const int out = warp_argmax(rest0, rest1, best);
-      const float worst = key_value(last), reach = 4.0f * tau + 2.4e-7f * finite_abs(worst);
+      const float worst = key_value(last);
+      float reach = 4.0f * tau + 2.4e-7f * finite_abs(worst), two_taus = 2.0f * tau;
+      if (ratios) {
+        // e^x is off by its logit's error and by a few 2^-24 |x| (x: the logit less the largest one), relative to its size; a sum's |x| is
+        // that of its larger part, no more than |log(sum / largest score)| + 1 and, weighted, as much again for the smaller part.  The
+        // last part: scores too small for fp32.
+        const float rel = delta + 1e-6f + 2e-7f * fminf(1.0f - __logf(fmaxf(worst / smax, 1e-38f)), 110.0f);
+        reach = rel * (worst + key_value(best)) + 1e-36f;
+        two_taus = 0.0f;                           // (the floors below are relative too)
+      }
       if (worst - key_value(best) <= reach) {
         // The last group that stays and the first one left out are too close.  If they are the only ones at the border, the scores that
         // their sums may be made of are evaluated; a third group there: everything.
@@ -191,12 +206,18 @@ __device__ __forceinline__ void choose_experts(const ScoredRouter& r, const Lane
         } else {
           d.in = in;
           d.out = out;
-          const float floor_in = __shfl_sync(0xffffffffu, in < 32 ? second0 : second1, in & 31) - 2.0f * tau;
-          const float floor_out = __shfl_sync(0xffffffffu, out < 32 ? second0 : second1, out & 31) - 2.0f * tau;
+          const float shrink = ratios ? 1.0f - 2.0f * (delta + 3e-5f) : 1.0f;
+          const float floor_in = __shfl_sync(0xffffffffu, in < 32 ? second0 : second1, in & 31) * shrink - two_taus;
+          const float floor_out = __shfl_sync(0xffffffffu, out < 32 ? second0 : second1, out & 31) * shrink - two_taus;
           auto part_of = [&](bool there, int e, float c) { return there && ((e / per == in && c >= floor_in) || (e / per == out && c >= floor_out)); };
           d.settled = uint64_t(__ballot_sync(0xffffffffu, part_of(v1, lane + 32, c1))) << 32 | __ballot_sync(0xffffffffu, part_of(v0, lane, c0));
         }
       }
+    }
+    if (!r.select_bias) {
+      k0 = v0 ? order_key(l0) : 0u;
+      k1 = v1 ? order_key(l1) : 0u;
+      tau = delta;
     }
     if (!((kept >> bias.group0) & 1ull)) k0 = 0u;
     if (!((kept >> bias.group1) & 1ull)) k1 = 0u;
@@ -233,8 +254,6 @@ __device__ __forceinline__ void choose_experts(const ScoredRouter& r, const Lane
     }
     d.chosen = chosen;
     d.which = which;
-    // scores of a softmax share their denominator: exact differences need every logit
-    if (!r.sigmoid && !by_logit) d.full = 1;
     d.settled = d.full ? (E == 64 ? ~0ull : (1ull << E) - 1ull) : d.settled | which;
     return;
   }
@@ -310,7 +329,7 @@ __device__ __noinline__ void choose_exactly(const ScoredRouter& r, double l0, do
       for (int o = 16; o > 0; o >>= 1) lm = fmax(lm, __shfl_xor_sync(0xffffffffu, lm, o));
       c0 = v0 ? exp(l0 - lm) : 0.0;
       c1 = v1 ? exp(l1 - lm) : 0.0;
-      const double den = warp_sum_f64(c0 + c1);
+      const double den = r.select_bias ? warp_sum_f64(c0 + c1) : 1.0;
       c0 /= den;
       c1 /= den;
     }
@@ -354,6 +373,10 @@ __device__ __noinline__ void choose_exactly(const ScoredRouter& r, double l0, do
       if (lane == (g & 31)) { if (g < 32) g0 = 0ull; else g1 = 0ull; }
       eligible |= ((1ull << per) - 1ull) << (g * per);
     }
+    if (!r.select_bias) {
+      k0 = v0 ? order_key(l0) : 0ull;
+      k1 = v1 ? order_key(l1) : 0ull;
+    }
     if (!((eligible >> lane) & 1ull)) k0 = 0ull;
     if (!((eligible >> (lane + 32)) & 1ull)) k1 = 0ull;
   }
@@ -367,8 +390,11 @@ __device__ __noinline__ void choose_exactly(const ScoredRouter& r, double l0, do
   }
 }
 
-// One token in doubt (a warp), its logits evaluated.  false: the border between groups falls differently, so all of its logits are needed.
-template <int kTokens>
+// One token in doubt (a warp), its logits evaluated.  false: all of its logits are needed, since the border between groups falls differently,
+// or since biased scores of a softmax are closer than the error of the fp32 denominator, which they share: an error in it moves a
+// difference of scores in proportion to the difference of what it divides, so that this is rare.
+// kBiased: biased scores of a softmax.
+template <bool kBiased, int kTokens>
 __device__ __forceinline__ bool settle(const ScoredRouter& r, int64_t t0, const RouteDoubts<kTokens>& q, int i, double* s_c, int lane) {
   const Doubt& d = q.d[i];
   const int k = r.k;
@@ -378,37 +404,54 @@ __device__ __forceinline__ bool settle(const ScoredRouter& r, int64_t t0, const 
     choose_exactly(r, l0, l1, s_c, lane, slot0, slot1);
   } else {
     const bool m0 = (d.settled >> lane) & 1ull, m1 = (d.settled >> (lane + 32)) & 1ull;
-    double c0 = l0, c1 = l1;                       // exact scores of the settled experts (sigmoid), or their logits
+    // exact scores of the settled experts (a softmax's with the fp32 denominator), or their logits; what a softmax's denominator divides
+    double c0 = l0, c1 = l1, e0 = 0.0, e1 = 0.0;
+    const double den_rel = double(d.den_rel) * double(d.inv_den);
+    // c, e and d, f: scores and what they are without the bias and the denominator
+    auto open = [&](double c, double e, double d, double f) {
+      if (isinf(c) || isinf(d)) return false;      // (an expert barred by -inf)
+      const double margin = den_rel * fabs(e - f) + 1e-14 * (fabs(c) + fabs(d));
+      return e != f && !(fabs(c - d) > margin);
+    };
+    bool unsure = false;
     if (r.select_bias || r.n_groups > 1) {
 #pragma unroll 1
       for (int h = 0; h < 2; ++h) {
         if (!(h ? m1 : m0)) continue;
-        const double c = 1.0 / (1.0 + exp(-(h ? l1 : l0))) + (r.select_bias ? double(r.select_bias[lane + 32 * h]) : 0.0);
-        (h ? c1 : c0) = c;
+        const double e = exp(!kBiased && r.sigmoid ? -(h ? l1 : l0) : (h ? l1 : l0) - double(d.l_max));
+        const double bias = kBiased || r.select_bias ? double(r.select_bias[lane + 32 * h]) : 0.0;
+        (h ? c1 : c0) = !kBiased && r.sigmoid ? 1.0 / (1.0 + e) + bias : kBiased ? e * double(d.inv_den) + bias : e;
+        (h ? e1 : e0) = e;
       }
     }
     __syncwarp();
     if (d.in >= 0) {
       // the two largest of either group, among the settled ones
       const int per = r.per_group;
-      double a[2] = {-INFINITY, -INFINITY}, b[2] = {-INFINITY, -INFINITY};
+      double a[2] = {-INFINITY, -INFINITY}, b[2] = {-INFINITY, -INFINITY}, ea[2] = {0.0, 0.0}, eb[2] = {0.0, 0.0};
 #pragma unroll 1
       for (uint64_t m = d.settled; m; m &= m - 1) {
         const int e = __ffsll((long long)m) - 1, g = e / per;
         const double x = __shfl_sync(0xffffffffu, c0, e & 31), y = __shfl_sync(0xffffffffu, c1, e & 31), c = e < 32 ? x : y;
+        const double u = __shfl_sync(0xffffffffu, e0, e & 31), v = __shfl_sync(0xffffffffu, e1, e & 31), ec = e < 32 ? u : v;
 #pragma unroll
         for (int h = 0; h < 2; ++h)
           if (g == (h ? d.out : d.in)) {
-            b[h] = fmax(b[h], fmin(a[h], c));
-            a[h] = fmax(a[h], c);
+            // (which of a group's scores are its two largest may hang on the denominator too)
+            if (kBiased && (open(c, ec, a[h], ea[h]) || open(c, ec, b[h], eb[h]))) unsure = true;
+            if (c > a[h]) { b[h] = a[h]; eb[h] = ea[h]; a[h] = c; ea[h] = ec; }
+            else if (c > b[h]) { b[h] = c; eb[h] = ec; }
           }
       }
       const double in = per > 1 ? a[0] + b[0] : a[0], out = per > 1 ? a[1] + b[1] : a[1];
+      const double e_in = per > 1 ? ea[0] + eb[0] : ea[0], e_out = per > 1 ? ea[1] + eb[1] : ea[1];
       if (!(in > out || (in == out && d.in < d.out))) return false;
+      if (kBiased && open(in, e_in, out, e_out)) unsure = true;
     }
     // All others are where they belong: the experts in doubt share out the places that experts in doubt have, in their exact order.
     const bool w0 = (d.which >> lane) & 1ull, w1 = (d.which >> (lane + 32)) & 1ull;
-    const uint64_t k0 = order_key(c0), k1 = order_key(c1);     // an order of all values, NaN too: no two experts get one place
+    // (an order of all values, NaN too: no two experts get one place)
+    const uint64_t k0 = order_key(r.select_bias ? c0 : l0), k1 = order_key(r.select_bias ? c1 : l1);
     int rank0 = 0, rank1 = 0;                      // how many of them come before the lane's
 #pragma unroll 1
     for (uint64_t m = d.which; m; m &= m - 1) {
@@ -416,7 +459,13 @@ __device__ __forceinline__ bool settle(const ScoredRouter& r, int64_t t0, const 
       const uint64_t a = __shfl_sync(0xffffffffu, k0, e & 31), b = __shfl_sync(0xffffffffu, k1, e & 31), c = e < 32 ? a : b;
       rank0 += c > k0 || (c == k0 && e < lane) ? 1 : 0;
       rank1 += c > k1 || (c == k1 && e < lane + 32) ? 1 : 0;
+      if (kBiased) {
+        const double x = __shfl_sync(0xffffffffu, c0, e & 31), y = __shfl_sync(0xffffffffu, c1, e & 31), ce = e < 32 ? x : y;
+        const double u = __shfl_sync(0xffffffffu, e0, e & 31), v = __shfl_sync(0xffffffffu, e1, e & 31), ee = e < 32 ? u : v;
+        if ((w0 && e != lane && open(ce, ee, c0, e0)) || (w1 && e != lane + 32 && open(ce, ee, c1, e1))) unsure = true;
+      }
     }
+    if (kBiased && __any_sync(0xffffffffu, unsure)) return false;
     int place = 0;
 #pragma unroll 1
     for (int j = 0; j < k; ++j) {
@@ -438,6 +487,13 @@ __device__ __forceinline__ bool settle(const ScoredRouter& r, int64_t t0, const 
   if (slot0 >= 0) { r.idx[at + slot0] = lane; r.w[at + slot0] = p0 / div * r.scale; }
   if (slot1 >= 0) { r.idx[at + slot1] = lane + 32; r.w[at + slot1] = p1 / div * r.scale; }
   return true;
+}
+
+// A function of its own where few tokens pass (37 tokens: 7.2 us, 8.1 in line) and for biased scores of a softmax, whose code is in the way of
+// the others' (8192 tokens: 33.4 us with both in line or both called, 32.2 so).
+template <bool kBiased, int kTokens>
+__device__ __noinline__ bool settle_called(const ScoredRouter& r, int64_t t0, const RouteDoubts<kTokens>& q, int i, double* s_c, int lane) {
+  return settle<kBiased>(r, t0, q, i, s_c, lane);
 }
 
 __device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
@@ -512,6 +568,7 @@ __device__ __forceinline__ void choose_share(const ScoredRouter& r, int64_t t0, 
   if (cluster > 1) ptx::cluster_sync();            // nobody leaves while its sums are being read
   else __syncthreads();
   const int doubts = q.n;
+  const bool biased_softmax = !r.sigmoid && r.select_bias;
   if (doubts == 0) return;                         // uniform over the CTA
   // the logits in doubt, a warp each; then the tokens, a warp each.  A second time for tokens that need all their logits after all.
 #pragma unroll 1
@@ -538,7 +595,9 @@ __device__ __forceinline__ void choose_share(const ScoredRouter& r, int64_t t0, 
 #pragma unroll 1
       for (int i = warp; i < doubts; i += n_warps) {
         if (again && q.d[i].full != 2) continue;
-        if (!settle(r, t0, q, i, s_c[warp], lane)) {
+        const bool settled = biased_softmax ? settle_called<true>(r, t0, q, i, s_c[warp], lane)
+                             : kTokens <= 16 ? settle_called<false>(r, t0, q, i, s_c[warp], lane) : settle<false>(r, t0, q, i, s_c[warp], lane);
+        if (!settled) {
           more = true;
           __syncwarp();
           if (lane == 0) {
@@ -979,8 +1038,9 @@ mote_status_t launch_route_scored(const mote_router_t* R, const void* x, int64_t
   ScoredRouter r{};
   r.x = static_cast<const uint16_t*>(x); r.ldx = ldx; r.Wr = R->Wr; r.logit_bias = R->logit_bias; r.select_bias = R->select_bias;
   r.w_norm = static_cast<const float*>(R->packed) + 1;
-  r.T = T; r.d = R->d; r.E = R->E; r.k = R->k; r.sigmoid = R->scoring == MOTE_SCORE_SIGMOID; r.n_groups = R->n_groups;
-  r.per_group = R->E / R->n_groups; r.topk_groups = R->topk_groups; r.renorm = R->renorm != 0; r.w_f32 = R->w_dtype == MOTE_DTYPE_F32; r.scale = R->scale;
+  r.T = T; r.d = R->d; r.E = R->E; r.k = R->k; r.sigmoid = R->scoring == MOTE_SCORE_SIGMOID;
+  r.n_groups = R->topk_groups == R->n_groups ? 1 : R->n_groups;            // where all groups stay there is nothing to choose among them
+  r.per_group = R->E / r.n_groups; r.topk_groups = R->topk_groups; r.renorm = R->renorm != 0; r.w_f32 = R->w_dtype == MOTE_DTYPE_F32; r.scale = R->scale;
   r.idx = idx; r.w = w; r.logits = logits;
   if (!status) status = static_cast<uint32_t*>(const_cast<void*>(R->packed));
   const int ne = (R->E + 7) / 8;

@@ -156,6 +156,30 @@ def test_route_scored_padded_batches_and_tiny_tokens(mote, T, scoring, n_groups,
                 n_groups=n_groups, topk_groups=max(1, n_groups // 2))
 
 
+@pytest.mark.parametrize("T", [5, 40, 1200])
+@pytest.mark.parametrize("E,n_groups,topk_groups", [(32, 8, 3), (32, 4, 4), (40, 20, 7), (24, 2, 1)])
+def test_route_scored_softmax_groups_of_close_and_of_vanishing_scores(mote, T, E, n_groups, topk_groups):
+    """Without a bias only ratios of a softmax's scores count: pairs of experts, and with them pairs of groups, that differ in their last
+    bits; and logits so far apart that most scores vanish in fp32."""
+    d = 512
+    x = _randn(85, T, d)
+    x[1::2] *= 40.0
+    Wr = (_randn(86, E // 2, d) * 0.1).repeat(2, 1).contiguous()          # an expert's twin is in another group
+    Wr[E // 2:] += (torch.rand(E // 2, d, generator=_gen(87), device="cuda") - 0.5) * 2.0 ** -24
+    check_route(mote, x.bfloat16(), Wr, 4, scoring="softmax", n_groups=n_groups, topk_groups=topk_groups)
+
+
+@pytest.mark.parametrize("T", [3, 300, 1200])
+@pytest.mark.parametrize("n_groups,topk_groups", [(1, 1), (8, 3), (2, 1)])
+def test_route_scored_biased_softmax_scores_that_hang_on_the_denominator(mote, T, n_groups, topk_groups):
+    """A bias that takes the scores of one token away but for its own rounding: every difference is far below what fp32 can tell."""
+    E, d = 32, 512
+    x = _randn(88, 1, d).bfloat16().repeat(T, 1).contiguous()
+    Wr = _randn(89, E, d) * 0.05
+    sb = (-torch.softmax(x[:1].double() @ Wr.double().T, dim=1)[0]).float()
+    check_route(mote, x, Wr, 6, None, sb, scoring="softmax", n_groups=n_groups, topk_groups=topk_groups)
+
+
 def test_route_scored_strided_rows_and_empty_batches(mote):
     wide = _randn(15, 50, 640).bfloat16()
     Wr = _randn(16, 24, 320) * 0.02
