@@ -5,7 +5,7 @@
 // W [N, K] is bf16, or the RTN codes of mote_rtn_quant (INT8 / INT4) with one scale per row; fp32 accumulation, one rounding
 // to the output's type.
 //
-// Up to kStreamMaxTokens tokens the product is a weight stream, bound by HBM and, at these sizes, by how much is in flight: a CTA owns 16 rows
+// For few tokens the product is a weight stream, bound by HBM and, at these sizes, by how much is in flight: a CTA owns 16 rows
 // of W, its warps share K, and asynchronous copies bring weights and tokens to rings in shared memory, from where they feed warp-level
 // MMAs, the weights (codes are expanded in registers) as the A operand, the tokens as the 8-wide B operand.  Every weight byte is read once.
 // us from a cold L2 (GB/s of weights): 1 x 2048 x 11008 bf16 9.4 (4800), 1 x 11008 x 2048 bf16 10.0 (4530), 8 x 2048 x 11008 INT8 8.7 (2630);
@@ -50,6 +50,11 @@ template <int NT, int kBits, int kWarps>
 __global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) linear_stream_kernel(LinearArgs a, int n_tiles) {
   using R = StreamRing<NT, kBits, kWarps>;
   constexpr int kLane = kBits == 16 ? 8 : 16, kStep = 4 * kLane;
+  const int64_t t0 = int64_t(blockIdx.y) * (NT * 8);             // this CTA's tokens
+  a.T -= t0;
+  a.x += t0 * a.ldx;
+  if (a.res) a.res += t0 * a.ldr;
+  a.out = static_cast<char*>(a.out) + t0 * a.N * (a.out_f32 ? 4 : 2);
   extern __shared__ __align__(16) uint8_t s_dyn[];
   __shared__ float s_part[2][kWarps][NT * 4][32];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
@@ -70,7 +75,7 @@ __global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) linear_stream_kernel
   const uint4* ring = reinterpret_cast<const uint4*>(s_dyn) + warp_base;
   const uint32_t ring_addr = (uint32_t)__cvta_generic_to_shared(s_dyn) + warp_base * 16;
   pdl_wait();
-  if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = 0u;
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *a.status = 0u;
 
   // the step that is fetched next: its tile, its number in the warp's share, its place, its rows
   int f_tile = n > 0 ? (int)blockIdx.x : n_tiles, f_step = 0, f_place = 0;
@@ -194,15 +199,16 @@ static cudaError_t launch_stream_as(const LinearArgs& a, int tiles, cudaStream_t
   constexpr int smem = StreamRing<NT, kBits, kWarps>::kBytes;
   const cudaError_t e = set_max_dynamic_smem(once, linear_stream_kernel<NT, kBits, kWarps>, smem);
   if (e != cudaSuccess) return e;
-  return launch_pdl(linear_stream_kernel<NT, kBits, kWarps>, dim3(std::min(tiles, device_sm_count() * (16 / kWarps))), dim3(kWarps * 32), smem, stream,
-                    a, tiles);
+  const int groups = (int)((a.T + NT * 8 - 1) / (NT * 8)), slots = std::max(1, device_sm_count() * (16 / kWarps) / groups);
+  return launch_pdl(linear_stream_kernel<NT, kBits, kWarps>, dim3(std::min(tiles, slots), groups), dim3(kWarps * 32), smem, stream, a, tiles);
 }
 template <int NT, int kBits>
 static cudaError_t launch_stream_bits(const LinearArgs& a, cudaStream_t stream) {
   // A tile per SM: sixteen warps share its K (1 x 2048 x 11008: 10.4 us with eight).  More tiles: two CTAs of eight warps per SM, whose sums and
   // barriers fall apart in time (16 x 8960 x 1536: 8.3 us, 9.5 with sixteen).
   const int tiles = (int)((a.N + kStreamRows - 1) / kStreamRows);
-  return tiles <= device_sm_count() ? launch_stream_as<NT, kBits, 16>(a, tiles, stream) : launch_stream_as<NT, kBits, 8>(a, tiles, stream);
+  const int groups = (int)((a.T + NT * 8 - 1) / (NT * 8));
+  return tiles * groups <= device_sm_count() ? launch_stream_as<NT, kBits, 16>(a, tiles, stream) : launch_stream_as<NT, kBits, 8>(a, tiles, stream);
 }
 template <int NT>
 static cudaError_t launch_stream(const LinearArgs& a, int bits, cudaStream_t stream) {
@@ -229,14 +235,21 @@ __global__ void __launch_bounds__(256) linear_expand_kernel(const uint2* __restr
   }
 }
 
-// Two column tiles of tokens.  At 17 tokens the tensor-core product takes 7.1 us for 2560 x 2048, at 16 this one 4.4.
-constexpr int64_t kStreamMaxTokens = 16;
-
 static int linear_bits(const mote_linear_t* L) { return L->bits == 0 ? MOTE_SHARED_BF16 : L->bits; }
 static bool linear_shape_ok(const mote_linear_t* L) {
   const int bits = linear_bits(L);
   return (bits == MOTE_SHARED_BF16 || bits == MOTE_SHARED_INT8 || bits == MOTE_SHARED_INT4) && L->N >= 1 && L->N <= (1 << 24) && L->K >= 1 &&
          L->K <= 65536 && L->K % (bits == MOTE_SHARED_BF16 ? 8 : 16) == 0 && L->act >= MOTE_ACT_NONE && L->act <= MOTE_ACT_GELU_TANH;
+}
+// Up to 16 tokens go through the weight stream, two column tiles of them; more in groups of 16, whose weights come from the L2 after the first
+// one, while that costs less than the tensor-core product's longer way.  Codes, which that product needs expanded: always for two groups
+// (32 x 2048 x 11008, INT8: 17.7 us, expanded 22.2; 2048 x 2048: 5.1, 12.5), for three and four while the groups' products are few
+// (64 x 2048 x 2048: 8.3, 12.9; 64 x 1536 x 8960: 22.5, 16.4).  bf16: two and three groups of few products (32 x 2048 x 2048: 5.5, 8.1;
+// 48 x 2048 x 2048: 7.7, 8.5; 32 x 1536 x 8960: 12.9, 9.2).
+static bool takes_stream(const mote_linear_t* L, int64_t T) {
+  const int64_t groups = (T + 15) / 16, work = groups * L->N * L->K;
+  if (linear_bits(L) == MOTE_SHARED_BF16) return groups <= 1 || (groups <= 3 && work <= 13000000);
+  return groups <= 2 || (groups <= 4 && work <= 40000000);
 }
 static bool ranges_overlap(const void* a, size_t na, const void* b, size_t nb) {
   const uintptr_t pa = reinterpret_cast<uintptr_t>(a), pb = reinterpret_cast<uintptr_t>(b);
@@ -248,8 +261,8 @@ static bool ranges_overlap(const void* a, size_t na, const void* b, size_t nb) {
 extern "C" size_t mote_linear_workspace_bytes(const mote_linear_t* L, int64_t T_max) {
   using namespace mote;
   if (!L || !linear_shape_ok(L) || T_max < 0 || T_max > (int64_t(1) << 24)) return 0;
-  // status word; from kStreamMaxTokens on the codes as bf16
-  const bool expands = linear_bits(L) != MOTE_SHARED_BF16 && T_max > kStreamMaxTokens;
+  // status word; where the tensor-core product takes over, the codes as bf16
+  const bool expands = linear_bits(L) != MOTE_SHARED_BF16 && !takes_stream(L, T_max);
   return 256 + (expands ? round_up(size_t(L->N) * L->K * 2, 256) : 0);
 }
 
@@ -280,7 +293,7 @@ extern "C" mote_status_t mote_linear(const mote_linear_t* L, const void* x, int6
   a.res = static_cast<const uint16_t*>(residual); a.ldr = sr; a.out = out; a.N = L->N; a.K = (int)L->K; a.act = L->act;
   a.out_f32 = out_dtype == MOTE_DTYPE_F32; a.status = static_cast<uint32_t*>(ws);
   cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-  if (T <= kStreamMaxTokens) {
+  if (takes_stream(L, T)) {
     MOTE_CUDA_OK(T <= 8 ? launch_stream<1>(a, bits, stream) : launch_stream<2>(a, bits, stream));
     MOTE_LAUNCH_OK();
     return MOTE_OK;

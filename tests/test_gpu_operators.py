@@ -327,6 +327,21 @@ def test_linear(mote, T, N, K, bits):
     check_linear(mote, lin, Wd, b, x, act, None, torch.float32)
 
 
+@pytest.mark.parametrize("T,N,K,bits", [
+    (17, 3300, 2048, 16), (32, 4104, 2048, 16), (33, 2127, 2048, 16), (48, 2200, 2048, 16), (49, 129, 64, 16), (64, 40, 72, 16), (16, 5001, 2048, 16),
+    (31, 9001, 1040, 8), (32, 5000, 4096, 4), (33, 7000, 2048, 8), (47, 7000, 2048, 4), (48, 1100, 2048, 8), (49, 6000, 2048, 8), (64, 6000, 2048, 4),
+    (64, 515, 80, 8), (65, 130, 48, 8), (65, 515, 80, 4), (80, 40, 16, 8)])
+def test_linear_where_the_forms_meet(mote, T, N, K, bits):
+    """Numbers of tokens and sizes on either side of where the weight stream hands over to the tensor-core product; the rows behind the
+    last token stay."""
+    lin, Wd, b = make_linear(mote, N, K, bits, True, "silu", T + N)
+    x, residual = _randn(T + K, T, K).bfloat16(), _randn(N, T, N).bfloat16()
+    out = torch.full((T + 2, N), 5.0, device="cuda")
+    check_linear(mote, lin, Wd, b, x, "silu", residual, torch.float32, out=out[:T])
+    assert bool((out[T:] == 5.0).all())
+    check_linear(mote, lin, Wd, b, x, "silu")
+
+
 @pytest.mark.parametrize("T", [5, 200, 1500])
 @pytest.mark.parametrize("act", ["none", "relu", "silu", "gelu", "gelu_tanh"])
 def test_linear_activations_over_their_range(mote, T, act):
