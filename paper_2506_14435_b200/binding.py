@@ -343,7 +343,7 @@ class MoteLinear:
         self.tensors = dict(W=W, scale=sc, bias=b)
         self.struct = mote_linear_t(self.N, self.K, W.data_ptr(), bits, sc_ptr, b_ptr, ACTS[act])
         self._address = C.addressof(self.struct)
-        self._ws = None
+        self._ws = self._small_ws = None     # the smaller one stays: a captured graph may hold its address
         self._ws_T = -1                      # the workspace serves up to this many tokens
         self._ws_address = self._ws_bytes = 0
 
@@ -358,7 +358,8 @@ class MoteLinear:
             need = lib.mote_linear_workspace_bytes(C.byref(self.struct), T)
             if need == 0:
                 raise MoteError(2, "mote_linear_workspace_bytes")
-            if need > self._ws_bytes:
+            if need > self._ws_bytes:        # at most twice: without room for the codes as bf16, and with it
+                self._small_ws = self._ws
                 self._ws = torch.empty(need, dtype=torch.uint8, device=self.tensors["W"].device)
                 self._ws_address, self._ws_bytes = self._ws.data_ptr(), need
             self._ws_T = T

@@ -393,9 +393,10 @@ __device__ __noinline__ void choose_exactly(const ScoredRouter& r, double l0, do
 // One token in doubt (a warp), its logits evaluated.  false: all of its logits are needed, since the border between groups falls differently,
 // or since biased scores of a softmax are closer than the error of the fp32 denominator, which they share: an error in it moves a
 // difference of scores in proportion to the difference of what it divides, so that this is rare.
-// kBiased: biased scores of a softmax.
+// kBiased: biased scores of a softmax.  A function, called, with the router as a __grid_constant__ parameter, so that its address can be
+// handed on: 8192 x 2048 takes 30.2 us, in line 33.4 (registers), with a copy of the router on the stack 32.2.
 template <bool kBiased, int kTokens>
-__device__ __forceinline__ bool settle(const ScoredRouter& r, int64_t t0, const RouteDoubts<kTokens>& q, int i, double* s_c, int lane) {
+__device__ __noinline__ bool settle(const ScoredRouter& r, int64_t t0, const RouteDoubts<kTokens>& q, int i, double* s_c, int lane) {
   const Doubt& d = q.d[i];
   const int k = r.k;
   const double l0 = q.l[i][lane], l1 = q.l[i][lane + 32];
@@ -487,13 +488,6 @@ __device__ __forceinline__ bool settle(const ScoredRouter& r, int64_t t0, const 
   if (slot0 >= 0) { r.idx[at + slot0] = lane; r.w[at + slot0] = p0 / div * r.scale; }
   if (slot1 >= 0) { r.idx[at + slot1] = lane + 32; r.w[at + slot1] = p1 / div * r.scale; }
   return true;
-}
-
-// A function of its own where few tokens pass (37 tokens: 7.2 us, 8.1 in line) and for biased scores of a softmax, whose code is in the way of
-// the others' (8192 tokens: 33.4 us with both in line or both called, 32.2 so).
-template <bool kBiased, int kTokens>
-__device__ __noinline__ bool settle_called(const ScoredRouter& r, int64_t t0, const RouteDoubts<kTokens>& q, int i, double* s_c, int lane) {
-  return settle<kBiased>(r, t0, q, i, s_c, lane);
 }
 
 __device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
@@ -595,8 +589,7 @@ __device__ __forceinline__ void choose_share(const ScoredRouter& r, int64_t t0, 
 #pragma unroll 1
       for (int i = warp; i < doubts; i += n_warps) {
         if (again && q.d[i].full != 2) continue;
-        const bool settled = biased_softmax ? settle_called<true>(r, t0, q, i, s_c[warp], lane)
-                             : kTokens <= 16 ? settle_called<false>(r, t0, q, i, s_c[warp], lane) : settle<false>(r, t0, q, i, s_c[warp], lane);
+        const bool settled = biased_softmax ? settle<true>(r, t0, q, i, s_c[warp], lane) : settle<false>(r, t0, q, i, s_c[warp], lane);
         if (!settled) {
           more = true;
           __syncwarp();
@@ -631,7 +624,7 @@ constexpr int kScoredTokens = 16;
 // Lane (g, t) = (lane / 4, lane % 4) loads elements [32 * step + 8 * t, + 8) of token rows g and g + 8 and of router rows 8n + g;
 // the reduction index may be permuted as long as both operands are.
 template <int NE, bool kF32>
-__global__ void __launch_bounds__(kScoredWarps * 32) route_scored_kernel(ScoredRouter r, int cluster) {
+__global__ void __launch_bounds__(kScoredWarps * 32) route_scored_kernel(const __grid_constant__ ScoredRouter r, int cluster) {
   __shared__ union {
     float part[kScoredWarps][NE * 4][32];
     struct { RouteDoubts<kScoredTokens> doubt; double c[kScoredWarps][64]; } late;
@@ -790,7 +783,7 @@ static_assert(sizeof(TileLate) <= kTilePipe, "the choices' data fit over the sta
 constexpr int kTileSmem = 1024 + kTilePipe + kTileTokens * (kTilePitch + 1) * 4 + (int)sizeof(TileBarriers);
 
 __global__ void __launch_bounds__(kTileThreads, 1)
-route_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w, ScoredRouter r, int cluster, int experts,
+route_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ ScoredRouter r, int cluster, int experts,
                   int terms, int stages, uint32_t* status) {
   using namespace ptx;
   extern __shared__ uint8_t smem_raw[];

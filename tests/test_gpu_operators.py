@@ -404,6 +404,21 @@ def test_operators_on_a_side_stream_and_in_graphs(mote):
 
 
 # ------------------------------------------------------------------------------------------------ the layer with a scored router
+@pytest.mark.parametrize("bits", [8, 4])
+def test_a_captured_projection_keeps_its_workspace_when_longer_batches_come(mote, bits):
+    lin, Wd, b = make_linear(mote, 512, 256, bits, True, "silu", 91)
+    x = _randn(92, 8, 256).bfloat16()
+    want = check_linear(mote, lin, Wd, b, x, "silu")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = mote.mote_linear(lin, x)
+    check_linear(mote, lin, Wd, b, _randn(93, 200, 256).bfloat16(), "silu")      # needs a larger one
+    others = [torch.ones(64, device="cuda") for _ in range(64)]                  # would take the place of the smaller one
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and all(bool((t == 1.0).all()) for t in others)
+
+
 @pytest.mark.parametrize("path", ["auto", "simt", "tensor", "stream"])
 @pytest.mark.parametrize("T", [1, 24, 40, 700])
 def test_moe_forward_scored_against_the_oracle(mote, T, path):
