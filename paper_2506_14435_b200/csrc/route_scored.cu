@@ -66,12 +66,26 @@ __device__ __forceinline__ float finite_abs(float v) { return fabsf(v) < INFINIT
 // only, and fetching it takes time too.  (Four or eight lanes to a token, 16 or 8 experts to a lane: 20 000 cycles a token, and no
 // faster for the 64 tokens that a CTA has in a long batch.)
 // ------------------------------------------------------------------------------------------------
-// The entry with the largest key of 64 (lane, and lane + 32 in the second slot), of equal ones the lower number.  Key 0: none.
-__device__ __forceinline__ int warp_argmax(uint32_t k0, uint32_t k1, uint32_t& best) {
-  best = __reduce_max_sync(0xffffffffu, max(k0, k1));
-  const unsigned b0 = __ballot_sync(0xffffffffu, k0 == best), b1 = __ballot_sync(0xffffffffu, k1 == best);
-  return b0 ? __ffs(b0) - 1 : 31 + __ffs(b1);
-}
+// Up to 64 entries, two to a lane, the larger one first; key 0: none.
+struct Entries {
+  uint32_t hi, lo;
+  int hi_id, lo_id;
+  __device__ __forceinline__ Entries(uint32_t k0, uint32_t k1, int lane) {
+    const bool swap = k1 > k0;
+    hi = swap ? k1 : k0; hi_id = swap ? lane + 32 : lane;
+    lo = swap ? k0 : k1; lo_id = swap ? lane : lane + 32;
+  }
+  // takes out the one with the largest key (of equal ones any: they are in doubt, but for -inf, whose keys differ)
+  __device__ __forceinline__ int take(uint32_t& best, int lane) {
+    best = __reduce_max_sync(0xffffffffu, hi);
+    const int from = __ffs(__ballot_sync(0xffffffffu, hi == best)) - 1;
+    const int id = __shfl_sync(0xffffffffu, hi_id, from);
+    if (lane == from) { hi = lo; hi_id = lo_id; lo = 0u; }
+    return id;
+  }
+};
+// order_key, and -inf ordered by index (decided, where other equal values are in doubt)
+__device__ __forceinline__ uint32_t entry_key(float v, int id) { return order_key(v) - (v == -INFINITY ? (uint32_t)id : 0u); }
 
 // What is known of a token whose choice the fp32 scores leave open.
 struct Doubt {
@@ -148,7 +162,7 @@ __device__ __forceinline__ void choose_experts(const ScoredRouter& r, const Lane
   const float c0 = (by_logit ? l0 : p0) + bias.s0, c1 = (by_logit ? l1 : p1) + bias.s1;
   // bound on the error of c: of the logit through the score's slope, of expf and the division, of adding the bias
   float tau = (by_logit ? delta : r.sigmoid ? 0.25f * delta + 4.8e-7f : delta < 0.5f ? smax * (2.0f * delta * (1.0f + 2.0f * delta) + 4e-6f) : 1e30f) + 1.2e-7f * bias.select_max;
-  uint32_t k0 = v0 ? order_key(c0) : 0u, k1 = v1 ? order_key(c1) : 0u, best;
+  uint32_t k0 = v0 ? entry_key(c0, lane) : 0u, k1 = v1 ? entry_key(c1, lane + 32) : 0u, best;
   d.full = 0;
   d.which = d.settled = 0ull;
   d.in = d.out = -1;
@@ -170,21 +184,20 @@ __device__ __forceinline__ void choose_experts(const ScoredRouter& r, const Lane
         a = fmaxf(a, v);
       }
       const float second = per > 1 ? b : a;
-      const uint32_t key = order_key(per > 1 ? a + b : a);
+      const uint32_t key = entry_key(per > 1 ? a + b : a, g);
       if (g < 32) { g0 = key; second0 = second; } else { g1 = key; second1 = second; }
     }
     uint64_t kept = 0ull;
-    uint32_t rest0 = g0, rest1 = g1, last = 0u;
+    uint32_t last = 0u;
     int in = 0;
+    Entries groups(g0, g1, lane);
 #pragma unroll 1
     for (int j = 0; j < r.topk_groups; ++j) {
-      in = warp_argmax(rest0, rest1, last);
-      if (lane == in) rest0 = 0u;
-      if (lane + 32 == in) rest1 = 0u;
+      in = groups.take(last, lane);
       kept |= 1ull << in;
     }
     if (r.topk_groups < G) {
-      const int out = warp_argmax(rest0, rest1, best);
+      const int out = groups.take(best, lane);
       const float worst = key_value(last);
       float reach = 4.0f * tau + 2.4e-7f * finite_abs(worst), two_taus = 2.0f * tau;
       if (ratios) {
@@ -215,54 +228,60 @@ __device__ __forceinline__ void choose_experts(const ScoredRouter& r, const Lane
       }
     }
     if (!r.select_bias) {
-      k0 = v0 ? order_key(l0) : 0u;
-      k1 = v1 ? order_key(l1) : 0u;
+      k0 = v0 ? entry_key(l0, lane) : 0u;
+      k1 = v1 ? entry_key(l1, lane + 32) : 0u;
       tau = delta;
     }
     if (!((kept >> bias.group0) & 1ull)) k0 = 0u;
     if (!((kept >> bias.group1) & 1ull)) k1 = 0u;
   }
-  // The k largest.  A lane keeps the place of its experts and the key of the choice before (all choices before an expert's are larger
-  // still, so that one is the closest).
-  int slot0 = k, slot1 = k;
-  uint32_t rest0 = k0, rest1 = k1, prev = 0u, before0 = 0u, before1 = 0u;
+  // The k largest: lane j keeps the j-th and its key.
+  Entries rest(k0, k1, lane);
+  uint32_t key = 0u;
+  int expert = 0;
 #pragma unroll 1
   for (int j = 0; j < k; ++j) {
-    const int e = warp_argmax(rest0, rest1, best);
-    if (lane == e) { slot0 = j; before0 = prev; rest0 = 0u; }
-    if (lane + 32 == e) { slot1 = j; before1 = prev; rest1 = 0u; }
-    prev = best;
+    const int e = rest.take(best, lane);
+    if (lane == j) { key = best; expert = e; }
   }
-  if (slot0 == k) before0 = prev;
-  if (slot1 == k) before1 = prev;
-  // closer to the choice before than the errors allow?  (key 0: cannot be taken; the first choice has none before it; equal -inf are decided)
-  auto is_near = [&](uint32_t key, int slot, uint32_t before) {
+  // Closer to the choice before than the errors allow?  All choices before that one are larger still; those not taken follow the last one.
+  // (equal -inf are decided)
+  auto is_near = [&](uint32_t key, uint32_t before) {
     const float c = key_value(key);
-    return key != 0u && slot > 0 && c > -INFINITY && key_value(before) - c <= 2.0f * tau;
+    return key != 0u && c > -INFINITY && key_value(before) - c <= 2.0f * tau;
   };
-  const bool near0 = is_near(k0, slot0, before0), near1 = is_near(k1, slot1, before1);
-  if (__any_sync(0xffffffffu, near0 || near1) || d.full || d.in >= 0) {
+  const uint32_t before = __shfl_up_sync(0xffffffffu, key, 1);
+  const bool near = lane > 0 && is_near(key, before), near_hi = is_near(rest.hi, best);
+  if (__any_sync(0xffffffffu, near || near_hi) || d.full || d.in >= 0) {
     // those experts, and the choices before them
-    uint64_t which = uint64_t(__ballot_sync(0xffffffffu, near1)) << 32 | __ballot_sync(0xffffffffu, near0), chosen = 0ull;
-    const unsigned places = __reduce_or_sync(0xffffffffu, (near0 ? 1u << (slot0 - 1) : 0u) | (near1 ? 1u << (slot1 - 1) : 0u));
-#pragma unroll 1
-    for (int j = 0; j < k; ++j) {
-      const unsigned b0 = __ballot_sync(0xffffffffu, slot0 == j), b1 = __ballot_sync(0xffffffffu, slot1 == j);
-      const int e = b0 ? __ffs(b0) - 1 : 31 + __ffs(b1);
-      chosen |= uint64_t(e) << (6 * j);
-      if ((places >> j) & 1u) which |= 1ull << e;
-    }
-    d.chosen = chosen;
-    d.which = which;
+    const int prev = __shfl_up_sync(0xffffffffu, expert, 1), last = __shfl_sync(0xffffffffu, expert, k - 1);
+    uint64_t which = 0ull;
+    if (near) which |= 1ull << expert | 1ull << prev;
+    if (near_hi) which |= 1ull << rest.hi_id | 1ull << last;
+    if (is_near(rest.lo, best)) which |= 1ull << rest.lo_id;
+    const uint64_t chosen = lane < k ? uint64_t(expert) << (6 * lane) : 0ull;
+    auto all_of = [](uint64_t m) {
+      return uint64_t(__reduce_or_sync(0xffffffffu, uint32_t(m >> 32))) << 32 | __reduce_or_sync(0xffffffffu, uint32_t(m));
+    };
+    d.chosen = all_of(chosen);
+    d.which = which = all_of(which);
     d.settled = d.full ? (E == 64 ? ~0ull : (1ull << E) - 1ull) : d.settled | which;
     return;
   }
+  const float a = __shfl_sync(0xffffffffu, p0, expert & 31), b = __shfl_sync(0xffffffffu, p1, expert & 31);
+  const float p = lane < k ? (expert < 32 ? a : b) : 0.0f;
   float mul = r.scale;
-  if (r.renorm) mul *= rcp_approx(fmaxf(warp_sum((slot0 < k ? p0 : 0.0f) + (slot1 < k ? p1 : 0.0f)), 1e-20f));
-  int32_t* idx = r.idx + token * k;
-  float* w = r.w + token * k;
-  if (slot0 < k) { idx[slot0] = lane; w[slot0] = p0 * mul; }
-  if (slot1 < k) { idx[slot1] = lane + 32; w[slot1] = p1 * mul; }
+  if (r.renorm) {
+    static_assert(MOTE_MAX_TOPK <= 8, "the choice in lanes 0 to 7");
+    float sum = p;
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    mul *= rcp_approx(fmaxf(sum, 1e-20f));
+  }
+  if (lane < k) {
+    r.idx[token * k + lane] = expert;
+    r.w[token * k + lane] = p * mul;
+  }
 }
 
 // A logit in 64 bits, by four warps a quarter each: its latency is what a long batch waits for.
