@@ -498,8 +498,13 @@ def mote_moe_forward(layer: MoteLayer, x: torch.Tensor, residual=None, out=None,
 
 def mote_moe_forward_scored(layer: MoteLayer, router: MoteRouter, x: torch.Tensor, residual=None, out=None, taps: dict | None = None):
     """mote_moe_forward with `router` (mote_route_scored) in the place of the layer's own."""
+    for t, name in ((x, "x"), (residual, "residual"), (out, "out")):
+        if t is not None and (t.dtype is not torch.bfloat16 or t.dim() != 2 or tuple(t.shape) != (x.shape[0], layer.d)):
+            raise ValueError(f"{name}: expected bfloat16 [T, {layer.d}]")
     _need_cuda(x, residual, out)
     _here(router.device)
+    if any(t is not None and t.get_device() != router.device for t in (x, residual, out, layer.tensors["Wr"])):
+        raise ValueError("expected the layer, its router and the tensors on one device")
     T = x.shape[0]
     if out is None:
         out = torch.empty_like(x)

@@ -156,6 +156,18 @@ def test_route_scored_padded_batches_and_tiny_tokens(mote, T, scoring, n_groups,
                 n_groups=n_groups, topk_groups=max(1, n_groups // 2))
 
 
+@pytest.mark.parametrize("T", [3, 500])
+@pytest.mark.parametrize("scoring", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("E,n_groups,topk_groups,k", [(16, 4, 2, 4), (40, 40, 9, 7), (50, 50, 8, 8), (64, 2, 1, 8), (36, 12, 11, 8)])
+def test_route_scored_groups_with_barred_logits(mote, T, scoring, E, n_groups, topk_groups, k):
+    """A logit_bias of -inf gives a score of zero: whole groups of them tie at zero, and are chosen only where no others are left."""
+    x = _randn(94, T, 128).bfloat16()
+    lb = torch.zeros(E, device="cuda")
+    lb[2:E - 5] = -float("inf")
+    check_route(mote, x, _randn(95, E, 128) * 0.1, k, lb, None, scoring=scoring, n_groups=n_groups, topk_groups=topk_groups)
+    check_route(mote, x, _randn(95, E, 128) * 0.1, k, lb, _randn(96, E) * 0.05, scoring=scoring, n_groups=n_groups, topk_groups=topk_groups)
+
+
 @pytest.mark.parametrize("T", [5, 40, 1200])
 @pytest.mark.parametrize("E,n_groups,topk_groups", [(32, 8, 3), (32, 4, 4), (40, 20, 7), (24, 2, 1)])
 def test_route_scored_softmax_groups_of_close_and_of_vanishing_scores(mote, T, E, n_groups, topk_groups):
@@ -178,6 +190,49 @@ def test_route_scored_biased_softmax_scores_that_hang_on_the_denominator(mote, T
     Wr = _randn(89, E, d) * 0.05
     sb = (-torch.softmax(x[:1].double() @ Wr.double().T, dim=1)[0]).float()
     check_route(mote, x, Wr, 6, None, sb, scoring="softmax", n_groups=n_groups, topk_groups=topk_groups)
+
+
+# The same where there is work enough for the tcgen05 kernel, on whole and partial tiles.
+@pytest.mark.parametrize("w_dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T,d", [(905, 1400), (2003, 5000), (1024, 4096)])
+@pytest.mark.parametrize("opt", ROUTES, ids=lambda o: "-".join(f"{k}{v}" for k, v in o.items()))
+def test_route_scored_long(mote, T, d, opt, w_dtype):
+    test_route_scored(mote, T, d, opt, w_dtype)
+
+
+@pytest.mark.parametrize("scoring,n_groups,bias", [("softmax", 1, False), ("sigmoid", 1, True), ("sigmoid", 8, True), ("softmax", 8, True), ("softmax", 8, False)])
+def test_route_scored_long_close_scores(mote, scoring, n_groups, bias):
+    test_route_scored_close_scores_are_told_apart_in_64_bits(mote, 2500, scoring, n_groups, bias)
+
+
+@pytest.mark.parametrize("scoring", ["softmax", "sigmoid"])
+def test_route_scored_long_equal_scores(mote, scoring):
+    test_route_scored_equal_scores_go_to_the_lower_index(mote, 6600, scoring)
+
+
+def test_route_scored_long_any_values(mote):
+    test_route_scored_takes_any_values_without_leaving_the_experts(mote, 39100)
+
+
+@pytest.mark.parametrize("scoring,n_groups,lb,sb", [("softmax", 1, False, False), ("sigmoid", 8, False, True), ("sigmoid", 8, True, False), ("softmax", 4, True, True)])
+def test_route_scored_long_padded_batches(mote, scoring, n_groups, lb, sb):
+    test_route_scored_padded_batches_and_tiny_tokens(mote, 2600, scoring, n_groups, lb, sb)
+
+
+@pytest.mark.parametrize("E,n_groups,topk_groups", [(32, 8, 3), (32, 4, 4), (40, 20, 7)])
+def test_route_scored_long_softmax_groups(mote, E, n_groups, topk_groups):
+    test_route_scored_softmax_groups_of_close_and_of_vanishing_scores(mote, 4900, E, n_groups, topk_groups)
+
+
+@pytest.mark.parametrize("n_groups,topk_groups", [(1, 1), (8, 3), (2, 1)])
+def test_route_scored_long_biased_softmax(mote, n_groups, topk_groups):
+    test_route_scored_biased_softmax_scores_that_hang_on_the_denominator(mote, 4900, n_groups, topk_groups)
+
+
+@pytest.mark.parametrize("scoring", ["softmax", "sigmoid"])
+def test_route_scored_long_barred(mote, scoring):
+    test_route_scored_groups_with_barred_logits(mote, 9800, scoring, 64, 2, 1, 8)
+    test_route_scored_barred_experts(mote, 19600, scoring)
 
 
 def test_route_scored_strided_rows_and_empty_batches(mote):
@@ -445,6 +500,20 @@ def test_moe_forward_scored_against_the_oracle(mote, T, path):
     assert np.linalg.norm(got - ref["out"]) / np.linalg.norm(ref["out"]) <= REL_FRO_TOL
     idx, w, _ = mote.mote_route_scored(router, x)
     assert torch.equal(idx, taps["topk_idx"]) and torch.equal(w, taps["topk_w"])
+
+
+def test_moe_forward_scored_refuses_other_shapes_and_takes_empty_batches(mote):
+    wl = synth.custom("scored", 128, 256, 8, 2, 4, 4301, w_std=0.08)
+    layer = mote.MoteLayer.from_master(synth.master_layer(wl))
+    router = mote.MoteRouter(_randn(97, 8, 128) * 0.05, 2)
+    x = _randn(98, 4, 128).bfloat16()
+    for bad in (dict(x=x.float()), dict(x=x[:, :64].contiguous()), dict(x=x, residual=x[:3]), dict(x=x, out=torch.empty(4, 128, device="cuda")),
+                dict(x=x.cpu()), dict(x=x[0])):
+        with pytest.raises(ValueError):
+            mote.mote_moe_forward_scored(layer, router, **bad)
+    with pytest.raises(mote.MoteError):
+        mote.mote_moe_forward_scored(layer, mote.MoteRouter(_randn(97, 4, 128) * 0.05, 2), x)
+    assert mote.mote_moe_forward_scored(layer, router, x).shape == (4, 128)
 
 
 def test_a_block_as_it_is_used(mote):
