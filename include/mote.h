@@ -208,7 +208,7 @@ mote_status_t mote_route_stats(const float* logits, const int32_t* topk_idx, int
  *           mote_device_status, which stays until it is read
  *   x_bf16  in   [T, d] bf16, row stride ldx elements (ldx >= d, ldx % 8 == 0), 16-B aligned
  *   topk_idx out [T, k] int32;  topk_w out [T, k] float;  logits out [T, E] float or NULL
- * T = 0 is a no-op.  Errors: d % 8 != 0, d > 32768, E < 1, E > MOTE_MAX_EXPERTS, k < 1, k > E, k > MOTE_MAX_TOPK, n_groups not
+ * T = 0 is a no-op.  Errors: T > 2^24, d % 8 != 0, d > 32768, E < 1, E > MOTE_MAX_EXPERTS, k < 1, k > E, k > MOTE_MAX_TOPK, n_groups not
  * a divisor of E, topk_groups not in 1 .. n_groups, k > topk_groups * E / n_groups, unknown scoring, a scale that is not a
  * number -> ERR_SHAPE; ERR_DTYPE; ERR_NULL; ERR_ALIGN.
  */
@@ -358,7 +358,7 @@ mote_status_t mote_rms_norm(const void* x_bf16, int64_t T, int64_t d, float eps,
  *   res_out  out [T, d] contiguous of res_dtype, or NULL;  normed_out out [T, d] bf16 contiguous, or NULL; not both NULL
  * An output may take the place of an input of the same element size and layout; any other overlap of the ranges is refused.
  * All pointers 16-B aligned but for a gate with gate_cols = 1 (its element's size).
- * T = 0 is a no-op.  Errors: d % 8 != 0, d > 32768, eps < 0, gate_cols not 0, 1 or d, gate_tokens < 0, overlap -> ERR_SHAPE;
+ * T = 0 is a no-op.  Errors: T > 2^24, d % 8 != 0, d > 32768, eps < 0, gate_cols not 0, 1 or d, gate_tokens < 0, overlap -> ERR_SHAPE;
  * ERR_DTYPE; ERR_NULL; ERR_ALIGN.
  */
 typedef struct {
@@ -390,7 +390,7 @@ mote_status_t mote_block_norm(const mote_block_norm_t* N, const void* y_bf16, in
  *   ws        scratch, >= mote_linear_workspace_bytes(L, T), 256-B aligned; its first word is the device status of
  *             mote_device_status.  Contents need not be kept between calls; two calls that can run at the same time need two.
  * Pointers 16-B aligned.  N is arbitrary; K % 8 == 0 (codes: K % 16 == 0).
- * T = 0 is a no-op.  Errors: N or K out of range (N <= 2^24, K <= 65536), unknown bits or act, overlap -> ERR_SHAPE; ERR_DTYPE;
+ * T = 0 is a no-op.  Errors: T, N or K out of range (T, N <= 2^24, K <= 65536), unknown bits or act, overlap -> ERR_SHAPE; ERR_DTYPE;
  * ERR_NULL; ERR_ALIGN; ERR_WORKSPACE.
  */
 enum { MOTE_ACT_NONE = 0, MOTE_ACT_RELU = 1, MOTE_ACT_SILU = 2, MOTE_ACT_GELU = 3, MOTE_ACT_GELU_TANH = 4 };
