@@ -431,10 +431,10 @@ linear_umma_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
 // ------------------------------------------------------------------------------------------------
 // Host side
 // ------------------------------------------------------------------------------------------------
-// Which form and tile width: the least estimated time, in cycles.  The estimate's constants were fitted to times of all forms at 70
-// sizes (17 to 8192 tokens, 26 to 11008 rows, K 128 to 11008): the form that it names is 2.5 % slower than the best one on average and
-// 24 % at worst; 4096 x 11008 x 2048: pairs of 256 x 224, 126 us (single CTAs 136), 333 x 8960 x 1536: single CTAs of 192, 13 us (pairs
-// 16), 64 x 2048 x 2048: tiles of 64 split four ways, 8.5 us (whole 12).
+// Which form and tile width: the least estimated time, in cycles.  The estimate's constants were fitted to times of all forms at 79
+// sizes (17 to 8192 tokens, 26 to 11008 rows, K 128 to 11008): the form that it names is 0.9 % slower than the best one on average and
+// 16 % at worst (2048 x 2048 x 2048: pairs of 256, 18.1 us, single CTAs of 240 15.7).  Tokens x N x K: 4096 x 11008 x 2048: pairs of 256, 122 us
+// (single CTAs 133), 333 x 8960 x 1536: single CTAs of 192, 13.6 us (pairs 16), 64 x 2048 x 2048: tiles of 64 split four ways, 8.4 us (whole 10).
 struct LinearForm { int cg, bn, splits; };
 static LinearForm pick_form(int64_t T, int64_t N, int k_steps, int sms, const int (&clusters)[9]) {
   LinearForm best{1, 256, 1};
@@ -445,11 +445,11 @@ static LinearForm pick_form(int64_t T, int64_t N, int k_steps, int sms, const in
     if (workers < 1) return;
     const double rounds = double((items + workers - 1) / workers);
     const double active = double(std::min(items, workers)) * cg * splits;
-    // a step: four MMAs, the way of its operands from L2 (77 bytes a cycle for an SM, 9300 for all of them), or a stage's latency
+    // a step: four MMAs, the way of its operands from L2 (61 bytes a cycle for an SM, 9300 for all of them), or a stage's latency
     const double bytes = double(std::min<int64_t>(T, 128)) * 128 + double(bn / cg) * 128;
-    const double step = std::max({2.0 * bn, bytes / 77.0, bytes * active / 9300.0, 420.0});
+    const double step = std::max({2.0 * bn, bytes / 61.0, bytes * active / 9300.0, 420.0});
     const double main = double((k_steps + splits - 1) / splits) * step;
-    const double epilogue = 2000.0 + 24.0 * bn / splits + (splits > 1 ? 4700.0 + 23.0 * bn : 0.0);
+    const double epilogue = 1900.0 + 19.0 * bn / splits + (splits > 1 ? 2800.0 + 28.0 * bn : cg == 2 ? 4000.0 : 0.0);
     const double cost = main + epilogue + (rounds - 1) * (std::max(main, epilogue) + 1000.0);
     if (cost < best_cost) { best_cost = cost; best = {cg, bn, splits}; }
   };
