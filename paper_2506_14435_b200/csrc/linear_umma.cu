@@ -38,7 +38,7 @@ struct LinearTiles {
   int n_mt, n_nt;
   int rows_fast;                                 // items: weight tiles (0) or token tiles (1) change fastest
   int a_rows;                                    // rows of the token operand's box
-  int vec8, wide;                                // rows of out (and residual) on 16-byte boundaries; out on 32-byte ones
+  int wide;                                      // rows of out on 32-byte boundaries
 };
 
 struct __align__(8) LinearBarriers {
@@ -69,8 +69,9 @@ __device__ __forceinline__ void load_columns(const LinearArgs& a, int64_t col0, 
 }
 
 // The residual of 16 neighbouring columns of a row, where rows lie on 16-byte boundaries.
-__device__ __forceinline__ void load_residual(const LinearArgs& a, const LinearTiles& t, int64_t row, int64_t col, uint4 (&r)[2]) {
-  if (!a.res || !t.vec8 || row >= a.T) return;
+template <bool kOdd>
+__device__ __forceinline__ void load_residual(const LinearArgs& a, int64_t row, int64_t col, uint4 (&r)[2]) {
+  if (kOdd || !a.res || row >= a.T) return;
   const uint4* rp = reinterpret_cast<const uint4*>(a.res + row * a.ldr + col);
   if (col < a.N) r[0] = rp[0];
   if (col + 8 < a.N) r[1] = rp[1];
@@ -101,8 +102,36 @@ __device__ __forceinline__ void write_rows(const LinearArgs& a, int64_t row0, in
   __syncwarp();
 }
 
+// Brings the residual of `n` columns from col on, 32 rows from row0 on, to the warp's block, where the rows lie on any boundary: as they will
+// be stored, so that a lane takes its row's from where it then puts its results (fp32 results, of twice the size: from the upper half of
+// the row, behind the first 16 results).  2-byte loads, neighbouring lanes neighbouring columns (419 x 896 x 9660: 18.7 us; each lane its own
+// row's: 25.7).
+__device__ __forceinline__ void read_rows(const LinearArgs& a, int64_t row0, int64_t col, int n, uint32_t* stg, int lane) {
+  __syncwarp();
+  const int rows = (int)min(int64_t(32), a.T - row0);
+  const uint16_t* from = a.res + row0 * a.ldr + col + lane;
+  uint16_t* to = reinterpret_cast<uint16_t*>(stg + (a.out_f32 ? 16 : 0)) + lane;
+  const bool in0 = lane < n, in1 = lane + 32 < n;
+#pragma unroll 1
+  for (int r = 0; r < rows; r += 4) {
+    uint16_t v0[4], v1[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (in0 && r + i < rows) v0[i] = from[(r + i) * a.ldr];
+      if (in1 && r + i < rows) v1[i] = from[(r + i) * a.ldr + 32];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (in0) to[(r + i) * 2 * kLinPitch] = v0[i];
+      if (in1) to[(r + i) * 2 * kLinPitch + 32] = v1[i];
+    }
+  }
+  __syncwarp();
+}
+
 // Finishes 16 neighbouring columns of a warp's 32 rows (lane = row): scale, bias, activation, residual, one rounding.  Stored at once
 // where rows lie on 16-byte boundaries, else put at column `at` of the warp's block.
+template <bool kOdd>
 __device__ __forceinline__ void finish_columns(const LinearArgs& a, const LinearTiles& t, uint64_t (&z)[8], const uint4 (&res)[2], int64_t row0,
                                                int64_t col, const float* cols, uint32_t* stg, int at, int lane) {
   if (a.w_scale) {
@@ -124,17 +153,14 @@ __device__ __forceinline__ void finish_columns(const LinearArgs& a, const Linear
   apply_act16(z, a.act);
   const int64_t row = row0 + lane;
   if (a.res) {
-    if (t.vec8) {                                // a half that lies outside is not stored
+    if (!kOdd) {                                 // a half that lies outside is not stored
       const uint32_t w[8] = {res[0].x, res[0].y, res[0].z, res[0].w, res[1].x, res[1].y, res[1].z, res[1].w};
 #pragma unroll
       for (int j = 0; j < 8; ++j) z[j] = add_f32x2(z[j], f32x2_bits(w[j] << 16, w[j] & 0xFFFF0000u));
-    } else if (row < a.T) {
-      const uint16_t* rp = a.res + row * a.ldr + col;
+    } else {                                     // (columns and rows that are not there hold anything)
+      const uint32_t* w = stg + lane * kLinPitch + (a.out_f32 ? 16 : 0) + at / 2;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const uint32_t lo = col + 2 * j < a.N ? rp[2 * j] : 0u, hi = col + 2 * j + 1 < a.N ? rp[2 * j + 1] : 0u;
-        z[j] = add_f32x2(z[j], f32x2_bits(lo << 16, hi << 16));
-      }
+      for (int j = 0; j < 8; ++j) z[j] = add_f32x2(z[j], f32x2_bits(w[j] << 16, w[j] & 0xFFFF0000u));
     }
   }
   uint32_t w[16];                                // the values as stored: 16 words, or 8 of two bf16 each
@@ -154,7 +180,7 @@ __device__ __forceinline__ void finish_columns(const LinearArgs& a, const Linear
       w[j] = pack_bf16x2(lo, hi);
     }
   }
-  if (!t.vec8) {
+  if (kOdd) {
     if (a.out_f32) {
 #pragma unroll
       for (int j = 0; j < 16; ++j) stg[lane * kLinPitch + at + j] = w[j];
@@ -196,7 +222,8 @@ struct Ring {
   }
 };
 
-template <int CG, bool kSplit>
+// kOdd: rows of out (or residual) without 16-byte boundaries.  (A kernel of its own: as a branch it costs the others 3 %.)
+template <int CG, bool kSplit, bool kOdd>
 __global__ void __launch_bounds__(kLinThreads, 1)
 linear_umma_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b, const LinearArgs a, const LinearTiles t) {
   static_assert(CG == 1 || !kSplit, "K is split over single CTAs");
@@ -205,7 +232,7 @@ linear_umma_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
   uint8_t* smem_gen = smem_raw + (smem_base - smem_u32(smem_raw));
   const uint32_t stage_b = uint32_t(t.bn / CG) * 128;
   const uint32_t stage_bytes = kLinStageA + stage_b;
-  uint32_t* staging = reinterpret_cast<uint32_t*>(smem_gen + kLinPipeBytesOdd);      // used where t.vec8 is not set
+  uint32_t* staging = reinterpret_cast<uint32_t*>(smem_gen + kLinPipeBytesOdd);      // kOdd
   float* column_data = reinterpret_cast<float*>(smem_gen + kLinPastPipe);
   LinearBarriers* bars = reinterpret_cast<LinearBarriers*>(smem_gen + kLinPastPipe + kLinColumns);
   volatile int* abort_flag = &bars->abort_flag;
@@ -316,21 +343,24 @@ linear_umma_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
       const int n = row0 < a.T ? (int)max(int64_t(0), min(int64_t(min(share, t.bn - part * share)), a.N - col0)) : 0;
       if (n > 0) load_columns(a, col0, n, cols, lane);
       uint4 res[2];
-      if (n > 0) load_residual(a, t, row0 + lane, col0, res);
+      if (n > 0) load_residual<kOdd>(a, row0 + lane, col0, res);
+      const bool block_res = kOdd && a.res;                     // the residual comes through the warp's block
+      if (block_res && n > 0) read_rows(a, row0, col0, min(room, n), stg, lane);
       if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->tmem_full[buf]), (local >> 1) & 1, abort_flag))) break;
       tc_fence_after();
       int put = 0;
 #pragma unroll 1
       for (int c = 0; c < n; c += 16) {
+        if (block_res && put == 0 && c > 0) read_rows(a, row0, col0 + c, min(room, n - c), stg, lane);
         uint32_t r[16];
         tmem_ld_32x32b_x16(t_row + c, r);
-        if (c > 0) load_residual(a, t, row0 + lane, col0 + c, res);
+        if (c > 0) load_residual<kOdd>(a, row0 + lane, col0 + c, res);
         tmem_wait_ld();
         uint64_t z[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) z[j] = f32x2_bits(r[2 * j], r[2 * j + 1]);
-        finish_columns(a, t, z, res, row0, col0 + c, cols + c, stg, put, lane);
-        if (!t.vec8) {
+        finish_columns<kOdd>(a, t, z, res, row0, col0 + c, cols + c, stg, put, lane);
+        if (kOdd) {
           put += 16;
           if (put == room || c + 16 >= n) {
             write_rows(a, row0, col0 + c + 16 - put, min(put, n - (c + 16 - put)), stg, lane);
@@ -384,7 +414,8 @@ linear_umma_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
 #pragma unroll 1
       for (int c = 0; c < n; c += 16) {
         uint4 res[2];
-        load_residual(a, t, row0 + lane, col0 + c, res);
+        load_residual<kOdd>(a, row0 + lane, col0 + c, res);
+        if (kOdd && a.res && put == 0) read_rows(a, row0, col0 + c, min(room, n - c), stg, lane);
         uint64_t z[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) z[j] = 0ull;
@@ -398,8 +429,8 @@ linear_umma_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
             z[j] = add_f32x2(z[j], f32x2(lo, hi));
           }
         }
-        finish_columns(a, t, z, res, row0, col0 + c, cols + c, stg, put, lane);
-        if (!t.vec8) {
+        finish_columns<kOdd>(a, t, z, res, row0, col0 + c, cols + c, stg, put, lane);
+        if (kOdd) {
           put += 16;
           if (put == room || c + 16 >= n) {
             write_rows(a, row0, col0 + c + 16 - put, min(put, n - (c + 16 - put)), stg, lane);
@@ -464,13 +495,21 @@ static LinearForm pick_form(int64_t T, int64_t N, int k_steps, int sms, const in
   return best;
 }
 
-template <int CG, bool kSplit>
+template <int CG, bool kSplit, bool kOdd>
 static cudaError_t launch_form(const CUtensorMap& ta, const CUtensorMap& tb, const LinearArgs& a, const LinearTiles& t, int grid, int cluster,
                                cudaStream_t stream) {
   static PerDeviceOnce once;
-  const cudaError_t e = set_max_dynamic_smem(once, linear_umma_kernel<CG, kSplit>, kLinSmem);
+  const cudaError_t e = set_max_dynamic_smem(once, linear_umma_kernel<CG, kSplit, kOdd>, kLinSmem);
   if (e != cudaSuccess) return e;
-  return launch_ex(linear_umma_kernel<CG, kSplit>, dim3(grid), dim3(kLinThreads), kLinSmem, stream, true, cluster, ta, tb, a, t);
+  return launch_ex(linear_umma_kernel<CG, kSplit, kOdd>, dim3(grid), dim3(kLinThreads), kLinSmem, stream, true, cluster, ta, tb, a, t);
+}
+
+template <bool kOdd>
+static cudaError_t launch_any(const LinearForm& f, const CUtensorMap& ta, const CUtensorMap& tb, const LinearArgs& a, const LinearTiles& t, int items,
+                              int sms, cudaStream_t stream) {
+  return f.splits > 1 ? launch_form<1, true, kOdd>(ta, tb, a, t, items * f.splits, f.splits, stream)
+         : f.cg == 2  ? launch_form<2, false, kOdd>(ta, tb, a, t, 2 * std::min(items, sms / 2), 2, stream)
+                      : launch_form<1, false, kOdd>(ta, tb, a, t, std::min(items, sms), 1, stream);
 }
 
 mote_status_t launch_linear_umma(const LinearArgs& a, cudaStream_t stream) {
@@ -478,10 +517,10 @@ mote_status_t launch_linear_umma(const LinearArgs& a, cudaStream_t stream) {
   LinearTiles t{};
   t.k_steps = (a.K + 63) / 64;
   static PerDeviceOnce split_once;               // its shared-memory limit has to be set before the query
-  if (set_max_dynamic_smem(split_once, linear_umma_kernel<1, true>, kLinSmem) != cudaSuccess) return MOTE_ERR_CUDA;
+  if (set_max_dynamic_smem(split_once, linear_umma_kernel<1, true, false>, kLinSmem) != cudaSuccess) return MOTE_ERR_CUDA;
   static ResidentClusters resident;
   int clusters[9] = {};
-  for (int c = 2; c <= 8; c *= 2) clusters[c] = resident.get(linear_umma_kernel<1, true>, kLinThreads, kLinSmem, c);
+  for (int c = 2; c <= 8; c *= 2) clusters[c] = resident.get(linear_umma_kernel<1, true, false>, kLinThreads, kLinSmem, c);
   const LinearForm f = pick_form(a.T, a.N, t.k_steps, sms, clusters);
   t.bn = f.bn; t.splits = f.splits;
   t.n_mt = (int)((a.T + 128 * f.cg - 1) / (128 * f.cg));
@@ -490,15 +529,13 @@ mote_status_t launch_linear_umma(const LinearArgs& a, cudaStream_t stream) {
   // the smaller operand's tiles change fastest: its whole stays in L2, the larger one is read from HBM once
   t.rows_fast = a.T <= a.N;
   t.a_rows = f.cg == 1 ? (int)std::min<int64_t>(128, (a.T + 7) / 8 * 8) : 128;
-  t.vec8 = a.N % 8 == 0 && (!a.res || a.ldr % 8 == 0);
-  t.stages = std::min(kLinMaxStages, (t.vec8 ? kLinPipeBytes : kLinPipeBytesOdd) / (kLinStageA + f.bn / f.cg * 128));
+  const bool odd = a.N % 8 != 0 || (a.res && a.ldr % 8 != 0);
+  t.stages = std::min(kLinMaxStages, (odd ? kLinPipeBytesOdd : kLinPipeBytes) / (kLinStageA + f.bn / f.cg * 128));
   t.wide = a.N % 16 == 0 && (reinterpret_cast<uintptr_t>(a.out) & 31u) == 0;
   CUtensorMap ta, tb;
   if (!make_operand_map(&ta, a.x, a.T, a.K, a.ldx, t.a_rows) || !make_operand_map(&tb, a.W, a.N, a.K, a.K, f.bn / f.cg)) return MOTE_ERR_CUDA;
   const int items = t.n_mt * t.n_nt;
-  const cudaError_t e = f.splits > 1 ? launch_form<1, true>(ta, tb, a, t, items * f.splits, f.splits, stream)
-                        : f.cg == 2  ? launch_form<2, false>(ta, tb, a, t, 2 * std::min(items, sms / 2), 2, stream)
-                                     : launch_form<1, false>(ta, tb, a, t, std::min(items, sms), 1, stream);
+  const cudaError_t e = odd ? launch_any<true>(f, ta, tb, a, t, items, sms, stream) : launch_any<false>(f, ta, tb, a, t, items, sms, stream);
   if (e != cudaSuccess) return MOTE_ERR_CUDA;
   MOTE_LAUNCH_OK();
   return MOTE_OK;

@@ -459,6 +459,19 @@ def test_operators_on_a_side_stream_and_in_graphs(mote):
 
 
 # ------------------------------------------------------------------------------------------------ the layer with a scored router
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("T,N,K", [(333, 1001, 512), (300, 515, 4096), (70, 37, 8192), (1500, 2051, 256), (4100, 130, 64), (129, 7, 1024)])
+def test_linear_residual_on_any_boundary(mote, T, N, K, bits):
+    lin, Wd, b = make_linear(mote, N, K, bits, True, "gelu_tanh", 101)
+    x, wide = _randn(102, T, K).bfloat16(), (_randn(103, T, N + 3) * 2.0).bfloat16()
+    rows = wide[:, :N]
+    check_linear(mote, lin, Wd, b, x, "gelu_tanh", rows, torch.float32)
+    want = check_linear(mote, lin, Wd, b, x, "gelu_tanh", rows)
+    place = rows.contiguous()
+    got = mote.mote_linear(lin, x, residual=place, out=place)
+    assert got is place and torch.equal(got, want)
+
+
 @pytest.mark.parametrize("bits", [8, 4])
 def test_a_captured_projection_keeps_its_workspace_when_longer_batches_come(mote, bits):
     lin, Wd, b = make_linear(mote, 512, 256, bits, True, "silu", 91)
