@@ -5,8 +5,9 @@
 //   groups: the topk_groups groups with the largest (sum of the two largest c) stay;  the k largest c among them are taken
 //
 // The choice is the one of exact arithmetic, whatever the order of the sums: scores are computed in fp32 with a bound on
-// their error, and a token whose choice lies within the bound has the scores concerned evaluated once more in 64 bits
-// (a few tokens in a thousand; see Doubt).  So all paths, batch sizes and splits give the same experts.
+// their error, and a token whose choice lies within the bound has the scores concerned evaluated once more in 64 bits (see
+// Doubt; one token in a hundred of normal ones, more where logits lie close together, all where saturated scores make
+// more than kMaxBorder groups alike).  So all paths, batch sizes and splits give the same experts.
 //
 // Logits: one cluster of CTAs per 16 tokens.  Each warp takes a part of the width and multiplies 16 tokens by all experts with
 // warp-level bf16 MMAs; an fp32 router weight is split exactly into three bf16 terms (8 + 8 + 8 significand bits), so every
@@ -34,12 +35,39 @@ struct ScoredRouter {
 };
 
 // ------------------------------------------------------------------------------------------------
-// Error bounds.  A product is exact, so a logit is off by the roundings of its partial sums, which are no larger than |x|_2 |w|_2
-// (Cauchy-Schwarz).  An MMA truncates what it adds up, hence sums of one step only (32 or 64 elements of the width) are left to it; they
-// join the others by additions rounded to nearest.  Truncation takes off a part of a logit that is the same for all experts; what is
-// left was at most 2^-22.2 |x|_2 |w|_2 over 10^7 logits of normal, outlier and one-signed tokens, widths 256 to 32768 (rms 2^-25.4 and less).
+// Error bounds.  A product is exact, so a logit is off by what its additions lose.  Sums are bounded by sum |x_i w_i| <= |x|_2 |w|_2, for the
+// parts of the width together too (Cauchy-Schwarz), so a bound relative to a part's own norms holds for the whole.  In units of 2^-24:
+//   * A tensor-core instruction brings its 16 products and the sum so far to one scale, cuts each off 25 bits below the largest, and cuts
+//     the result to 24 bits (found by sums of 1 and n products of 2^-j, the same for mma.sync and tcgen05): 17 addends of half a
+//     unit, a result of two: 10.5 for 16 elements.  The weights' upper terms come last; what the middle and lower ones, 2^-7 and less of
+//     the weights, lose on the way is 0.4.
+//   * A sum by warp-level MMAs is of 16 elements, and two of them are added (1); one by tcgen05.mma is of 32, two instructions (21), and two
+//     of them are added (1).  These sums are added up with compensation (Kahan: 2, however many they are).  The parts of warps and CTAs
+//     meet in pairs of floats (Knuth's two-sum: of second order), which become one float where a CTA hands over its part and as the
+//     logit: 2.
+//   * The addition of logit_bias: 1, and 2 of the bias.
+// Products of random signs lose one or two in all.
 // ------------------------------------------------------------------------------------------------
-constexpr float kLogitEps = 5.4e-07f;                  // 2^-21, and an eighth for the roundings where sums meet
+constexpr float kUnit = 1.0f / 16777216.0f;
+constexpr float kWarpLogitEps = 17.5f * kUnit, kTileLogitEps = 27.0f * kUnit;      // 16.9 and 26.4, and what the norms may be off by
+
+// hi + lo += v, lo being what the additions to hi have lost (exactly, for each).
+__device__ __forceinline__ void two_sum(float& hi, float& lo, float v) {
+  const float s = __fadd_rn(hi, v), part = __fsub_rn(s, hi);
+  lo = __fadd_rn(lo, __fadd_rn(__fsub_rn(hi, __fsub_rn(s, part)), __fsub_rn(v, part)));
+  hi = s;
+}
+__device__ __forceinline__ uint64_t sub_f32x2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(b), "l"(f32x2(-1.0f, -1.0f)), "l"(a));
+  return d;
+}
+// sum += v, two at a time; over: what `sum` holds too much.
+__device__ __forceinline__ void compensated_add(uint64_t& sum, uint64_t& over, uint64_t v) {
+  const uint64_t y = sub_f32x2(v, over), t = add_f32x2(sum, y);
+  over = sub_f32x2(sub_f32x2(t, sum), y);
+  sum = t;
+}
 
 // order-preserving integer images of floats and doubles; never 0, which marks an entry that cannot be taken
 __device__ __forceinline__ uint32_t order_key(float v) {
@@ -87,11 +115,13 @@ struct Entries {
 // order_key, and -inf ordered by index (decided, where other equal values are in doubt)
 __device__ __forceinline__ uint32_t entry_key(float v, int id) { return order_key(v) - (v == -INFINITY ? (uint32_t)id : 0u); }
 
+constexpr int kMaxBorder = 8;                      // groups at the border that are told apart by the scores concerned
+
 // What is known of a token whose choice the fp32 scores leave open.
 struct Doubt {
   int token;                                       // number within the CTA's tokens
   int full;                                        // 1: all logits and the whole choice anew
-  int in, out;                                     // the groups on either side of the border, if they are too close; else -1
+  uint64_t border, kept;                           // groups too close to the border to tell which stay (none: 0); groups that the fp32 scores keep
   float l_max, inv_den, den_rel;                   // softmax: what is taken off the logits, 1 / denominator and the bound on its relative error
   uint64_t which;                                  // experts whose order is open
   uint64_t settled;                                // experts whose logits are evaluated in 64 bits: those, and the groups'
@@ -165,7 +195,7 @@ __device__ __forceinline__ void choose_experts(const ScoredRouter& r, const Lane
   uint32_t k0 = v0 ? entry_key(c0, lane) : 0u, k1 = v1 ? entry_key(c1, lane + 32) : 0u, best;
   d.full = 0;
   d.which = d.settled = 0ull;
-  d.in = d.out = -1;
+  d.border = 0ull;
   if (r.n_groups > 1) {
     const int G = r.n_groups, per = r.per_group;
     __syncwarp();
@@ -189,15 +219,11 @@ __device__ __forceinline__ void choose_experts(const ScoredRouter& r, const Lane
     }
     uint64_t kept = 0ull;
     uint32_t last = 0u;
-    int in = 0;
     Entries groups(g0, g1, lane);
 #pragma unroll 1
-    for (int j = 0; j < r.topk_groups; ++j) {
-      in = groups.take(last, lane);
-      kept |= 1ull << in;
-    }
+    for (int j = 0; j < r.topk_groups; ++j) kept |= 1ull << groups.take(last, lane);
     if (r.topk_groups < G) {
-      const int out = groups.take(best, lane);
+      groups.take(best, lane);
       const float worst = key_value(last);
       float reach = 4.0f * tau + 2.4e-7f * finite_abs(worst), two_taus = 2.0f * tau;
       if (ratios) {
@@ -209,21 +235,24 @@ __device__ __forceinline__ void choose_experts(const ScoredRouter& r, const Lane
         two_taus = 0.0f;                           // (the floors below are relative too)
       }
       if (worst - key_value(best) <= reach) {
-        // The last group that stays and the first one left out are too close.  If they are the only ones at the border, the scores that
-        // their sums may be made of are evaluated; a third group there: everything.
+        // The last group that stays and the first one left out are too close.  Of the groups around the border, the scores that their
+        // sums may be made of are evaluated; where those are many: everything.
         const float lo = key_value(best) - reach, hi = worst + reach;
         auto at_border = [&](uint32_t key) { return key != 0u && key_value(key) >= lo && key_value(key) <= hi; };
-        const int n = __popc(__ballot_sync(0xffffffffu, at_border(g0))) + __popc(__ballot_sync(0xffffffffu, at_border(g1)));
-        if (n > 2) {
+        d.border = uint64_t(__ballot_sync(0xffffffffu, at_border(g1))) << 32 | __ballot_sync(0xffffffffu, at_border(g0));
+        d.kept = kept;
+        if (__popcll(d.border) > kMaxBorder) {
           d.full = 1;
         } else {
-          d.in = in;
-          d.out = out;
           const float shrink = ratios ? 1.0f - 2.0f * (delta + 3e-5f) : 1.0f;
-          const float floor_in = __shfl_sync(0xffffffffu, in < 32 ? second0 : second1, in & 31) * shrink - two_taus;
-          const float floor_out = __shfl_sync(0xffffffffu, out < 32 ? second0 : second1, out & 31) * shrink - two_taus;
-          auto part_of = [&](bool there, int e, float c) { return there && ((e / per == in && c >= floor_in) || (e / per == out && c >= floor_out)); };
-          d.settled = uint64_t(__ballot_sync(0xffffffffu, part_of(v1, lane + 32, c1))) << 32 | __ballot_sync(0xffffffffu, part_of(v0, lane, c0));
+          second0 = second0 * shrink - two_taus;   // floors
+          second1 = second1 * shrink - two_taus;
+          auto part_of = [&](bool there, int g, float c) {
+            const float a = __shfl_sync(0xffffffffu, second0, g & 31), b = __shfl_sync(0xffffffffu, second1, g & 31);
+            return there && ((d.border >> g) & 1ull) && c >= (g < 32 ? a : b);
+          };
+          const bool part0 = part_of(v0, bias.group0, c0), part1 = part_of(v1, bias.group1, c1);
+          d.settled = uint64_t(__ballot_sync(0xffffffffu, part1)) << 32 | __ballot_sync(0xffffffffu, part0);
         }
       }
     }
@@ -252,7 +281,7 @@ __device__ __forceinline__ void choose_experts(const ScoredRouter& r, const Lane
   };
   const uint32_t before = __shfl_up_sync(0xffffffffu, key, 1);
   const bool near = lane > 0 && is_near(key, before), near_hi = is_near(rest.hi, best);
-  if (__any_sync(0xffffffffu, near || near_hi) || d.full || d.in >= 0) {
+  if (__any_sync(0xffffffffu, near || near_hi) || d.full || d.border) {
     // those experts, and the choices before them
     const int prev = __shfl_up_sync(0xffffffffu, expert, 1), last = __shfl_sync(0xffffffffu, expert, k - 1);
     uint64_t which = 0ull;
@@ -445,28 +474,40 @@ __device__ __noinline__ bool settle(const ScoredRouter& r, int64_t t0, const Rou
       }
     }
     __syncwarp();
-    if (d.in >= 0) {
-      // the two largest of either group, among the settled ones
-      const int per = r.per_group;
-      double a[2] = {-INFINITY, -INFINITY}, b[2] = {-INFINITY, -INFINITY}, ea[2] = {0.0, 0.0}, eb[2] = {0.0, 0.0};
+    if (d.border) {
+      // a lane for each group at the border: its sum, and what the sum is without the biases and the denominator
+      const int per = r.per_group, n = __popcll(d.border);
+      double sum = 0.0, e_sum = 0.0;
+      int group = 0, i = 0;
 #pragma unroll 1
-      for (uint64_t m = d.settled; m; m &= m - 1) {
-        const int e = __ffsll((long long)m) - 1, g = e / per;
-        const double x = __shfl_sync(0xffffffffu, c0, e & 31), y = __shfl_sync(0xffffffffu, c1, e & 31), c = e < 32 ? x : y;
-        const double u = __shfl_sync(0xffffffffu, e0, e & 31), v = __shfl_sync(0xffffffffu, e1, e & 31), ec = e < 32 ? u : v;
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-          if (g == (h ? d.out : d.in)) {
-            // (which of a group's scores are its two largest may hang on the denominator too)
-            if (kBiased && (open(c, ec, a[h], ea[h]) || open(c, ec, b[h], eb[h]))) unsure = true;
-            if (c > a[h]) { b[h] = a[h]; eb[h] = ea[h]; a[h] = c; ea[h] = ec; }
-            else if (c > b[h]) { b[h] = c; eb[h] = ec; }
-          }
+      for (uint64_t groups = d.border; groups; groups &= groups - 1, ++i) {
+        const int g = __ffsll((long long)groups) - 1;
+        // the two largest of the group, among the settled ones
+        double a = -INFINITY, b = -INFINITY, ea = 0.0, eb = 0.0;
+#pragma unroll 1
+        for (uint64_t m = d.settled & (per == 64 ? ~0ull : ((1ull << per) - 1ull) << (g * per)); m; m &= m - 1) {
+          const int e = __ffsll((long long)m) - 1;
+          const double x = __shfl_sync(0xffffffffu, c0, e & 31), y = __shfl_sync(0xffffffffu, c1, e & 31), c = e < 32 ? x : y;
+          const double u = __shfl_sync(0xffffffffu, e0, e & 31), v = __shfl_sync(0xffffffffu, e1, e & 31), ec = e < 32 ? u : v;
+          // (which of a group's scores are its two largest may hang on the denominator too)
+          if (kBiased && (open(c, ec, a, ea) || open(c, ec, b, eb))) unsure = true;
+          if (c > a) { b = a; eb = ea; a = c; ea = ec; }
+          else if (c > b) { b = c; eb = ec; }
+        }
+        if (lane == i) { group = g; sum = per > 1 ? a + b : a; e_sum = per > 1 ? ea + eb : ea; }
       }
-      const double in = per > 1 ? a[0] + b[0] : a[0], out = per > 1 ? a[1] + b[1] : a[1];
-      const double e_in = per > 1 ? ea[0] + eb[0] : ea[0], e_out = per > 1 ? ea[1] + eb[1] : ea[1];
-      if (!(in > out || (in == out && d.in < d.out))) return false;
-      if (kBiased && open(in, e_in, out, e_out)) unsure = true;
+      // those that stay must come before those that do not
+      const bool out = lane < n && !((d.kept >> group) & 1ull);
+      bool wrong = false;
+#pragma unroll 1
+      for (int j = 0; j < n; ++j) {
+        const int g = __shfl_sync(0xffffffffu, group, j);
+        const double s = __shfl_sync(0xffffffffu, sum, j), e = __shfl_sync(0xffffffffu, e_sum, j);
+        if (!out || !((d.kept >> g) & 1ull)) continue;
+        wrong |= !(s > sum || (s == sum && g < group));
+        if (kBiased && open(s, e, sum, e_sum)) unsure = true;
+      }
+      if (__any_sync(0xffffffffu, wrong)) return false;
     }
     // All others are where they belong: the experts in doubt share out the places that experts in doubt have, in their exact order.
     const bool w0 = (d.which >> lane) & 1ull, w1 = (d.which >> (lane + 32)) & 1ull;
@@ -520,7 +561,7 @@ __device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
 // n_warps - 1 choose; s_c: 64 doubles for each of them.
 template <int kTokens>
 __device__ __forceinline__ void choose_share(const ScoredRouter& r, int64_t t0, int rank, int cluster, int share, const float* part, int pitch,
-                                             const float* xx_part, RouteDoubts<kTokens>& q, double (*s_c)[64],
+                                             const float* xx_part, float logit_eps, RouteDoubts<kTokens>& q, double (*s_c)[64],
                                              int warp, int n_warps, int lane) {
   const int n = (int)min(int64_t(share), max(int64_t(0), r.T - t0 - rank * share));      // tokens of this CTA that are there
   if (warp < n_warps && warp < n) {
@@ -535,15 +576,18 @@ __device__ __forceinline__ void choose_share(const ScoredRouter& r, int64_t t0, 
       const int number = rank * share + i;
       const int64_t token = t0 + number;
       float l0 = 0.0f, l1 = 0.0f, xx = 0.0f;
-      if (cluster > 1) {                           // the parts' sums, rank by rank
+      if (cluster > 1) {
+        float lost0 = 0.0f, lost1 = 0.0f;                           // the parts' sums, rank by rank
         const uint32_t row = ptx::smem_u32(part + number * pitch), x_at = ptx::smem_u32(xx_part + number);
 #pragma unroll 2
         for (int c = 0; c < cluster; ++c) {
           const uint32_t far = ptx::map_to_rank(row, c);
-          l0 += ld_cluster_f32(far + 4 * e0);
-          l1 += ld_cluster_f32(far + 4 * e1);
+          two_sum(l0, lost0, ld_cluster_f32(far + 4 * e0));
+          two_sum(l1, lost1, ld_cluster_f32(far + 4 * e1));
           xx += ld_cluster_f32(ptx::map_to_rank(x_at, c));
         }
+        l0 += lost0;
+        l1 += lost1;
       } else {
         l0 = part[number * pitch + e0];
         l1 = part[number * pitch + e1];
@@ -557,7 +601,7 @@ __device__ __forceinline__ void choose_share(const ScoredRouter& r, int64_t t0, 
       }
       Doubt d;
       float p0, p1;
-      choose_experts(r, bias, token, l0, l1, kLogitEps * sqrt_approx(xx) * w_norm + 1.2e-7f * bias.logit_max, reinterpret_cast<float*>(s_c[warp]), d, p0, p1,
+      choose_experts(r, bias, token, l0, l1, logit_eps * sqrt_approx(xx) * w_norm + 1.2e-7f * bias.logit_max, reinterpret_cast<float*>(s_c[warp]), d, p0, p1,
                      lane);
       if (d.settled) {
         const bool zeros = xx == 0.0f;             // a token of zeros: its logits are the biases, there is nothing to evaluate
@@ -642,8 +686,10 @@ constexpr int kScoredTokens = 16;
 // NE: 8-expert column tiles (ceil(E / 8) rounded up to 1, 2, 4 or 8); kF32: type of the router weights.
 // Lane (g, t) = (lane / 4, lane % 4) loads elements [32 * step + 8 * t, + 8) of token rows g and g + 8 and of router rows 8n + g;
 // the reduction index may be permuted as long as both operands are.
-template <int NE, bool kF32>
-__global__ void __launch_bounds__(kScoredWarps * 32) route_scored_kernel(const __grid_constant__ ScoredRouter r, int cluster) {
+// kAlone: a CTA has its SM to itself, and registers for all sums of 64 experts (512 x 2048: 14.4 us, 16.6 with half of them); two share one
+// where CTAs are more (4096 x 256: 15.9 us, 20.5 one after the other).
+template <int NE, bool kF32, bool kAlone>
+__global__ void __launch_bounds__(kScoredWarps * 32, kAlone ? 1 : 2) route_scored_kernel(const __grid_constant__ ScoredRouter r, int cluster) {
   __shared__ union {
     float part[kScoredWarps][NE * 4][32];
     struct { RouteDoubts<kScoredTokens> doubt; double c[kScoredWarps][64]; } late;
@@ -661,9 +707,9 @@ __global__ void __launch_bounds__(kScoredWarps * 32) route_scored_kernel(const _
   const bool ga = t0 + g < r.T, gb = t0 + g + 8 < r.T;
   const uint16_t* xa = r.x + (ga ? t0 + g : 0) * r.ldx + t * 8;
   const uint16_t* xb = r.x + (gb ? t0 + g + 8 : 0) * r.ldx + t * 8;
-  float acc[NE][4];
+  uint64_t acc[NE][2], over[NE][2];
 #pragma unroll
-  for (int n = 0; n < NE; ++n) acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.0f;
+  for (int n = 0; n < NE; ++n) acc[n][0] = acc[n][1] = over[n][0] = over[n][1] = 0ull;
   float xxa = 0.0f, xxb = 0.0f;
   uint32_t bits_a = 0u, bits_b = 0u;
   const uint4 kZero = make_uint4(0u, 0u, 0u, 0u);
@@ -691,8 +737,8 @@ __global__ void __launch_bounds__(kScoredWarps * 32) route_scored_kernel(const _
 #pragma unroll
         for (int n = 0; n < NE; ++n) {
           const bool row = in && n * 8 + g < E;
-          // an MMA truncates what it adds up: a step's sum starts from zero and joins the others by a rounded addition
-          float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+          // an MMA truncates what it adds up: sums of 16 elements start from zero, the smallest terms first, and join the others outside
+          float pa[4] = {0.0f, 0.0f, 0.0f, 0.0f}, pb[4] = {0.0f, 0.0f, 0.0f, 0.0f};
           if (kF32) {
             float4 w0 = make_float4(0.f, 0.f, 0.f, 0.f), w1 = w0;
             if (row) {
@@ -709,20 +755,20 @@ __global__ void __launch_bounds__(kScoredWarps * 32) route_scored_kernel(const _
               mid[j] = __uint_as_float(__float_as_uint(r1) & 0xFFFF0000u);
               lo[j] = __fsub_rn(r1, mid[j]);
             }
-            mma_bf16_k16(part, ca.x, cb.x, ca.y, cb.y, upper_halves(hi[0], hi[1]), upper_halves(hi[2], hi[3]));
-            mma_bf16_k16(part, ca.z, cb.z, ca.w, cb.w, upper_halves(hi[4], hi[5]), upper_halves(hi[6], hi[7]));
-            mma_bf16_k16(part, ca.x, cb.x, ca.y, cb.y, upper_halves(mid[0], mid[1]), upper_halves(mid[2], mid[3]));
-            mma_bf16_k16(part, ca.z, cb.z, ca.w, cb.w, upper_halves(mid[4], mid[5]), upper_halves(mid[6], mid[7]));
-            mma_bf16_k16(part, ca.x, cb.x, ca.y, cb.y, upper_halves(lo[0], lo[1]), upper_halves(lo[2], lo[3]));
-            mma_bf16_k16(part, ca.z, cb.z, ca.w, cb.w, upper_halves(lo[4], lo[5]), upper_halves(lo[6], lo[7]));
+            mma_bf16_k16(pa, ca.x, cb.x, ca.y, cb.y, upper_halves(lo[0], lo[1]), upper_halves(lo[2], lo[3]));
+            mma_bf16_k16(pb, ca.z, cb.z, ca.w, cb.w, upper_halves(lo[4], lo[5]), upper_halves(lo[6], lo[7]));
+            mma_bf16_k16(pa, ca.x, cb.x, ca.y, cb.y, upper_halves(mid[0], mid[1]), upper_halves(mid[2], mid[3]));
+            mma_bf16_k16(pb, ca.z, cb.z, ca.w, cb.w, upper_halves(mid[4], mid[5]), upper_halves(mid[6], mid[7]));
+            mma_bf16_k16(pa, ca.x, cb.x, ca.y, cb.y, upper_halves(hi[0], hi[1]), upper_halves(hi[2], hi[3]));
+            mma_bf16_k16(pb, ca.z, cb.z, ca.w, cb.w, upper_halves(hi[4], hi[5]), upper_halves(hi[6], hi[7]));
           } else {
             uint4 w = kZero;
             if (row) w = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(r.Wr) + int64_t(n * 8 + g) * d + s * 32 + t * 8);
-            mma_bf16_k16(part, ca.x, cb.x, ca.y, cb.y, w.x, w.y);
-            mma_bf16_k16(part, ca.z, cb.z, ca.w, cb.w, w.z, w.w);
+            mma_bf16_k16(pa, ca.x, cb.x, ca.y, cb.y, w.x, w.y);
+            mma_bf16_k16(pb, ca.z, cb.z, ca.w, cb.w, w.z, w.w);
           }
-#pragma unroll
-          for (int i = 0; i < 4; ++i) acc[n][i] += part[i];
+          compensated_add(acc[n][0], over[n][0], add_f32x2(f32x2(pa[0], pa[1]), f32x2(pb[0], pb[1])));
+          compensated_add(acc[n][1], over[n][1], add_f32x2(f32x2(pa[2], pa[3]), f32x2(pb[2], pb[3])));
         }
         const uint32_t wa[4] = {ca.x, ca.y, ca.z, ca.w}, wb[4] = {cb.x, cb.y, cb.z, cb.w};
 #pragma unroll
@@ -746,14 +792,15 @@ __global__ void __launch_bounds__(kScoredWarps * 32) route_scored_kernel(const _
 #pragma unroll
   for (int n = 0; n < NE; ++n)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) sh.part[warp][n * 4 + i][lane] = acc[n][i];
+    for (int h = 0; h < 2; ++h)
+      unpack_f32x2(acc[n][h], sh.part[warp][n * 4 + 2 * h][lane], sh.part[warp][n * 4 + 2 * h + 1][lane]);
   __syncthreads();
   // fragment: value i of column tile n at lane (g, t) is token row g + 8*(i/2), expert 8n + 2t + (i&1)
   for (int v = warp; v < NE * 4; v += kScoredWarps) {
-    float z = sh.part[0][v][lane];
+    float z = sh.part[0][v][lane], z_lost = 0.0f;
 #pragma unroll
-    for (int w = 1; w < kScoredWarps; ++w) z += sh.part[w][v][lane];
-    s_logits[g + 8 * ((v & 3) >> 1)][(v >> 2) * 8 + 2 * t + (v & 1)] = z;
+    for (int w = 1; w < kScoredWarps; ++w) two_sum(z, z_lost, sh.part[w][v][lane]);
+    s_logits[g + 8 * ((v & 3) >> 1)][(v >> 2) * 8 + 2 * t + (v & 1)] = z + z_lost;
   }
   if (threadIdx.x < kScoredTokens) {
     float z = s_norm[0][threadIdx.x];
@@ -765,23 +812,23 @@ __global__ void __launch_bounds__(kScoredWarps * 32) route_scored_kernel(const _
   if (threadIdx.x == 0) sh.late.doubt.n = 0;
   if (cluster > 1) ptx::cluster_sync();
   else __syncthreads();
-  choose_share(r, t0, rank, cluster, kScoredTokens / cluster, &s_logits[0][0], NE * 8 + 1, s_xx, sh.late.doubt, sh.late.c, warp,
+  choose_share(r, t0, rank, cluster, kScoredTokens / cluster, &s_logits[0][0], NE * 8 + 1, s_xx, kWarpLogitEps, sh.late.doubt, sh.late.c, warp,
                kScoredWarps, lane);
 }
 
 // ------------------------------------------------------------------------------------------------
 // Logits of long batches: tcgen05.mma kind::f16, a tile of 128 tokens x all experts per cluster of CTAs that share the width.
 //
-// TMA brings 64 elements of the tokens and of the router's rows (its three bf16 terms, or its bf16 rows) to a stage.  A stage's 4 x terms
-// MMAs form a sum of their own in TMEM -- the tensor core truncates what it adds up, so sums are kept short -- and the epilogue warps
-// add it to fp32 sums in registers, rounded to nearest (eight such accumulators, so that neither side waits for the other).  Eight
+// TMA brings 64 elements of the tokens and of the router's rows (its three bf16 terms, or its bf16 rows) to a stage.  Either half of a
+// stage's 4 x terms MMAs forms a sum of its own in TMEM, the smallest terms first -- the tensor core truncates what it adds up, so sums are
+// kept short -- and the epilogue warps add both to pairs of fp32 sums in registers (four such accumulators, so that neither side waits for the other).  Eight
 // more warps read the tokens of the stage from shared memory for their norms.  Then as above: sums meet in distributed shared memory,
 // each CTA chooses for its share of the 128 tokens.
 //
 // Warps: 0 TMA producer, 1 MMA issuer, 2 TMEM owner, 4 to 19 epilogue (four per TMEM lane quarter, 16 experts each), 20 to 27 norms;
 // all 32 choose.
 //
-// 8192 x 2048, 64 experts in 8 groups, fp32 Wr: 29.4 us in a graph, where the bytes take 5.4.  About 11 us are the products: 655 KB of
+// 8192 x 2048, 64 experts in 8 groups, fp32 Wr: 29.1 us in a graph (27.7 with sums of 64 elements added without compensation, whose bound did not hold), where the bytes take 5.4.  About 11 us are the products: 655 KB of
 // operands an SM, three fifths of them the weights' terms, are 6 us at the 61 bytes a cycle that an SM gets, the rest is the start of the
 // pipeline.  7 are the choice, bound by instructions (710 a token, 64 tokens to an SM), 4 second evaluations, latency.
 // The kernel above, whose tokens are 16 to a cluster, takes 78.
@@ -791,7 +838,7 @@ constexpr int kTileWarps = 16, kTileNormWarps = 8, kTileThreads = 1024;
 constexpr int kTileStageA = kTileTokens * 128;
 constexpr int kTilePipe = 4 * (kTileStageA + 3 * 64 * 128);      // 160 KB: four stages with three terms of 64 experts, more with less
 constexpr int kTileMaxStages = 6;
-constexpr int kTileSums = 8;                                      // accumulators in TMEM, 64 columns each
+constexpr int kTileSums = 4;                                      // accumulators in TMEM, 2 x 64 columns each
 constexpr int kTilePitch = 65;
 
 struct __align__(8) TileBarriers {
@@ -831,7 +878,7 @@ route_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constan
     prefetch_tensormap(&tm_w);
   }
   if (warp == 2) {
-    tmem_alloc(smem_u32(&bars->tmem_base), 64 * kTileSums);
+    tmem_alloc(smem_u32(&bars->tmem_base), 128 * kTileSums);
     tmem_relinquish();
   }
   tc_fence_before();
@@ -872,10 +919,13 @@ route_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constan
       const uint64_t da = smem_desc_sw128(base + s * stage_bytes);
       if (elect_one()) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          for (int term = 0; term < terms; ++term)
-            mma_f16(tmem + a * 64, da + 2 * j, smem_desc_sw128(base + s * stage_bytes + kTileStageA + term * experts * 128) + 2 * j, idesc,
-                    j + term > 0 ? 1u : 0u);
+        for (int h = 0; h < 2; ++h)
+          for (int term = terms - 1; term >= 0; --term)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+              mma_f16(tmem + a * 128 + h * 64, da + 4 * h + 2 * j,
+                      smem_desc_sw128(base + s * stage_bytes + kTileStageA + term * experts * 128) + 4 * h + 2 * j, idesc,
+                      j > 0 || term < terms - 1 ? 1u : 0u);
         mma_commit(smem_u32(&bars->empty[s]));
         mma_commit(smem_u32(&bars->sum_full[a]));
       }
@@ -885,27 +935,34 @@ route_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constan
   } else if (warp >= 4 && warp < 4 + kTileWarps) {
     const int q = warp & 3, col = ((warp - 4) >> 2) * 16;
     const bool mine = col < experts;
-    float sum[16];
+    uint64_t sum[8], over[8];
 #pragma unroll
-    for (int j = 0; j < 16; ++j) sum[j] = 0.0f;
+    for (int j = 0; j < 8; ++j) sum[j] = over[j] = 0ull;
     for (int n = 0; n < ke - kb; ++n) {
       const int a = n % kTileSums;
       if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->sum_full[a]), (n / kTileSums) & 1, abort_flag))) break;
       tc_fence_after();
-      if (mine) {
-        uint32_t v[16];
-        tmem_ld_32x32b_x16(tmem + (uint32_t(q * 32) << 16) + a * 64 + col, v);
-        tmem_wait_ld();
+      if (mine)
 #pragma unroll
-        for (int j = 0; j < 16; ++j) sum[j] += __uint_as_float(v[j]);
-      }
+        for (int c = 0; c < 16; c += 8) {          // (8 columns of both sums at a time: registers)
+          uint32_t u[8], v[8];
+          tmem_ld_32x32b_x8(tmem + (uint32_t(q * 32) << 16) + a * 128 + col + c, u);
+          tmem_ld_32x32b_x8(tmem + (uint32_t(q * 32) << 16) + a * 128 + 64 + col + c, v);
+          tmem_wait_ld();
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            compensated_add(sum[c / 2 + j], over[c / 2 + j], add_f32x2(f32x2_bits(u[2 * j], u[2 * j + 1]), f32x2_bits(v[2 * j], v[2 * j + 1])));
+        }
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&bars->sum_empty[a]));
     }
     if (mine)
 #pragma unroll
-      for (int j = 0; j < 16; ++j) part[(q * 32 + lane) * kTilePitch + col + j] = sum[j];
+      for (int j = 0; j < 8; ++j) {
+        float* at = part + (q * 32 + lane) * kTilePitch + col + 2 * j;
+        unpack_f32x2(sum[j], at[0], at[1]);
+      }
   } else if (warp >= 4 + kTileWarps && warp < 4 + kTileWarps + kTileNormWarps) {
     // eight lanes read a token's 128 bytes (in any order), the warp four tokens of each quarter of the tile
     const int first = (warp - 4 - kTileWarps) * 4 + (lane >> 3);
@@ -947,12 +1004,12 @@ route_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constan
   if (threadIdx.x == 0) late->doubt.n = 0;
   if (warp == 2) {
     tc_fence_after();
-    tmem_dealloc(tmem, 64 * kTileSums);
+    tmem_dealloc(tmem, 128 * kTileSums);
   }
   if (cluster > 1) cluster_sync();
   else __syncthreads();
   if (threadIdx.x == 0 && *abort_flag) atomicExch(status, 1u);
-  choose_share(r, t0, rank, cluster, kTileTokens / cluster, part, kTilePitch, xx, late->doubt, late->c, warp, kTileThreads / 32, lane);
+  choose_share(r, t0, rank, cluster, kTileTokens / cluster, part, kTilePitch, xx, kTileLogitEps, late->doubt, late->c, warp, kTileThreads / 32, lane);
 }
 
 // What a router keeps beside its weights: [0] a device status word, [1] the largest 2-norm of a row (rounded up), and from byte 256 on an
@@ -1021,10 +1078,15 @@ static bool router_ok(const mote_router_t* R) {
          R->k <= R->topk_groups * (R->E / R->n_groups) && R->scale == R->scale;
 }
 
+template <int NE, bool kF32>
+static cudaError_t launch_scored_as(const ScoredRouter& r, unsigned grid, int cluster, cudaStream_t stream) {
+  return (int)grid <= device_sm_count()
+             ? launch_ex(route_scored_kernel<NE, kF32, true>, dim3(grid), dim3(kScoredWarps * 32), 0, stream, true, cluster, r, cluster)
+             : launch_ex(route_scored_kernel<NE, kF32, false>, dim3(grid), dim3(kScoredWarps * 32), 0, stream, true, cluster, r, cluster);
+}
 template <int NE>
 static cudaError_t launch_scored(const ScoredRouter& r, unsigned tiles, int cluster, cudaStream_t stream) {
-  return r.w_f32 ? launch_ex(route_scored_kernel<NE, true>, dim3(tiles * cluster), dim3(kScoredWarps * 32), 0, stream, true, cluster, r, cluster)
-                 : launch_ex(route_scored_kernel<NE, false>, dim3(tiles * cluster), dim3(kScoredWarps * 32), 0, stream, true, cluster, r, cluster);
+  return r.w_f32 ? launch_scored_as<NE, true>(r, tiles * cluster, cluster, stream) : launch_scored_as<NE, false>(r, tiles * cluster, cluster, stream);
 }
 
 static cudaError_t launch_tiles(const ScoredRouter& r, const CUtensorMap& tx, const CUtensorMap& tw, int experts, int terms, uint32_t* status,

@@ -1,0 +1,85 @@
+"""Inputs on which the operators around the experts (mote_route_scored, mote_block_norm, mote_linear) go wrong if a bound, a barred
+entry or a value that is not finite is not minded, against statements in 64 bits (oracle/mote_oracle.py) and sharp bounds."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import mote_oracle as O
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def mote():
+    import paper_2506_14435_b200 as m
+    return m
+
+
+def _randn(seed, *shape):
+    return torch.randn(shape, generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda")
+
+
+def _f64(t):
+    return None if t is None else t.detach().double().cpu().numpy()
+
+
+# ------------------------------------------------------------------------------------------------ scored router
+# A token and two router rows, 0 and 1, whose logits differ by a little in favour of row 0.  Its logit is one product of 1 and many
+# small ones, each lost to an adder that has the 1 already; row 1's is the product 1 + m 2^-23 alone.
+def spike_rows(kind, d):
+    small_x, small_w, first, last = {
+        # products of 2^-30, one after the other: 512 of them are 2^-21, each below half of the last place of 1
+        "chain": (2.0 ** -15, 2.0 ** -15, 0, d),
+        # products just below 2^-25 beside the 1, in one step of the tensor cores
+        "step": (1.9375 * 2.0 ** -13, 1.03125 * 2.0 ** -13, 0, 64),
+        # both
+        "all": (1.9375 * 2.0 ** -13, 1.03125 * 2.0 ** -13, 0, d),
+    }[kind]
+    x, a = np.zeros(d), np.zeros(d)
+    x[first:last], a[first:last] = small_x, small_w
+    x[0] = a[0] = 1.0
+    return x, a
+
+
+@pytest.mark.parametrize("tokens", [1, 20, 333, 9728])
+@pytest.mark.parametrize("d", [128, 2048, 8192, 32768])
+@pytest.mark.parametrize("kind", ["chain", "step", "all"])
+@pytest.mark.parametrize("E", [2, 64])
+def test_route_scored_small_products_beside_a_large_one(mote, kind, d, tokens, E):
+    x, a = spike_rows(kind, d)
+    gain = (x[1:] @ a[1:]) * 2.0 ** 23                    # what row 0 has over 1, in units of 2^-23
+    xt = torch.tensor(x, device="cuda").bfloat16()
+    assert np.array_equal(_f64(xt), x)
+    for m in sorted({max(1, round(gain * q)) for q in (0.1, 0.3, 0.5, 0.6, 0.7, 0.8, 0.9, 0.97, 1.03, 1.2)}):
+        Wr = torch.zeros(E, d, dtype=torch.float64)
+        Wr[:, 0] = -1.0
+        Wr[0] = torch.tensor(a)
+        Wr[1] = 0.0
+        Wr[1, 0] = 1.0 + m * 2.0 ** -23
+        Wt = Wr.cuda().float()
+        assert torch.equal(Wt.double().cpu(), Wr) and gain != m
+        xs = xt.repeat(tokens, 1)
+        xs[1::2] *= 4.0                                   # (an exact multiple: the same order)
+        for scoring, k in (("softmax", 1), ("sigmoid", 2)):
+            idx = mote.mote_route_scored(mote.MoteRouter(Wt, k, scoring=scoring), xs)[0]
+            want = [0, 1][:k] if gain > m else [1, 0][:k]
+            assert bool((idx.cpu() == torch.tensor(want, dtype=torch.int32)).all()), (m, gain, idx[:3].tolist())
+
+
+@pytest.mark.parametrize("d,E,w_dtype", [(2048, 64, torch.float32), (8192, 16, torch.float32), (32768, 8, torch.bfloat16), (32768, 64, torch.float32)])
+def test_route_scored_wide_tokens_get_the_same_experts_in_every_batch(mote, d, E, w_dtype):
+    """Pairs of rows that differ in their last bits, tokens of one sign with a leading channel: alone, in middle and in long batches
+    the choice of exact arithmetic."""
+    T = 9728
+    x = _randn(201, 64, d).abs()
+    x[::2, 0] *= 1000.0
+    x = x.bfloat16()
+    Wr = (_randn(202, E // 2, d).abs() * 0.02).repeat_interleave(2, dim=0)
+    Wr[1::2] += (torch.rand(E // 2, d, generator=torch.Generator("cuda").manual_seed(203), device="cuda") - 0.5) * (2.0 ** -27 if w_dtype == torch.float32 else 2.0 ** -16)
+    Wr = Wr.to(w_dtype).contiguous()
+    want = torch.from_numpy(O.route_scored(_f64(x), _f64(Wr), 4, scoring="sigmoid")["idx"])
+    r = mote.MoteRouter(Wr, 4, scoring="sigmoid")
+    long = mote.mote_route_scored(r, x.repeat(T // 64, 1))[0].cpu().view(-1, 64, 4)
+    assert bool((long == want).all())
+    assert torch.equal(mote.mote_route_scored(r, x)[0].cpu(), want)
+    assert torch.equal(mote.mote_route_scored(r, x[5:6])[0].cpu(), want[5:6])
