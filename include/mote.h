@@ -203,7 +203,9 @@ mote_status_t mote_route_stats(const float* logits, const int32_t* topk_idx, int
  * evaluated again in 64 bits (and compared in them), so the same token gets the same experts in every batch and on every path.
  * The bound counts every rounding, and what a tensor-core instruction cuts off as B200s were found to do it (25 bits below its
  * largest addend); it does not depend on d.  Logits must be finite in fp32.
- * logit_bias and select_bias may hold -inf: such an expert is chosen only where fewer than k others are left.
+ * logit_bias and select_bias may hold -inf: such an expert is chosen only where the groups that stay have fewer than k
+ * others, the lower index first.  A logit of -inf has a score of 0, to a group's sum too and where all logits are -inf
+ * (weights of 0 then), and comes after all others whatever its select_bias.
  *
  *   Wr      [E, d], w_dtype MOTE_DTYPE_F32 or MOTE_DTYPE_BF16, 16-B aligned; logit_bias, select_bias [E] float or NULL
  *   packed  output of mote_router_pack for this Wr, 256-B aligned; its first word is the device status of

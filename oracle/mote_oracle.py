@@ -409,7 +409,8 @@ def route_scored(x: np.ndarray, Wr: np.ndarray, k: int, *, scoring="softmax", lo
                  topk_groups=1, renorm=True, scale=1.0):
     """Router with softmax or sigmoid scores, a bias that takes part in the choice alone, groups and renormalised weights, fp64,
     token by token.  x [T, d] and Wr [E, d] as fp64 values of the stored ones.  Without select_bias the experts are ordered
-    by logit (scores grow with it), else by c = score + select_bias; a tie goes to the lower index."""
+    by logit (scores grow with it), else by c = score + select_bias, those with a logit of -inf last; a tie goes to the lower
+    index.  A logit of -inf has a score of 0, where all are -inf too."""
     T, E = x.shape[0], Wr.shape[0]
     l = x.astype(np.float64) @ Wr.astype(np.float64).T
     if logit_bias is not None:
@@ -418,8 +419,8 @@ def route_scored(x: np.ndarray, Wr: np.ndarray, k: int, *, scoring="softmax", lo
     per = E // n_groups
     for t in range(T):
         if scoring == "softmax":
-            e = np.exp(l[t] - l[t].max())
-            s = e / e.sum()
+            e = np.exp(l[t] - l[t].max()) if l[t].max() > -np.inf else np.zeros(E)
+            s = e / max(e.sum(), 1.0)
         else:
             with np.errstate(over="ignore"):
                 s = 1.0 / (1.0 + np.exp(-l[t]))
@@ -427,7 +428,7 @@ def route_scored(x: np.ndarray, Wr: np.ndarray, k: int, *, scoring="softmax", lo
         group = [sum(sorted(c[g * per:(g + 1) * per], reverse=True)[:2]) for g in range(n_groups)]
         kept = sorted(range(n_groups), key=lambda g: (-group[g], g))[:topk_groups]
         open_ = [e for e in range(E) if e // per in kept]
-        order = l[t] if select_bias is None else c
+        order = l[t] if select_bias is None else np.where(l[t] == -np.inf, -np.inf, c)
         pick = sorted(open_, key=lambda e: (-order[e], e))[:k]
         idx[t] = pick
         w[t] = scale * s[pick] / (max(s[pick].sum(), 1e-20) if renorm else 1.0)

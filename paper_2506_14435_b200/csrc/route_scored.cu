@@ -179,10 +179,10 @@ __device__ __forceinline__ void choose_experts(const ScoredRouter& r, const Lane
     p0 = rcp_approx(1.0f + __expf(-l0));
     p1 = rcp_approx(1.0f + __expf(-l1));
   } else {
-    const float lm = warp_max(fmaxf(v0 ? l0 : -INFINITY, v1 ? l1 : -INFINITY));
+    const float lm = fmaxf(warp_max(fmaxf(v0 ? l0 : -INFINITY, v1 ? l1 : -INFINITY)), -3.4e38f);      // (all barred: scores of 0)
     p0 = v0 ? __expf(l0 - lm) : 0.0f;
     p1 = v1 ? __expf(l1 - lm) : 0.0f;
-    smax = rcp_approx(warp_sum(p0 + p1));
+    smax = rcp_approx(fmaxf(warp_sum(p0 + p1), 1.0f));             // (1 is the largest one's part; less where all are barred)
     d.l_max = lm;
     d.inv_den = smax;
     d.den_rel = delta < 1.0f ? delta * (1.0f + delta) + 4e-6f : 1e30f;      // e^delta - 1
@@ -264,6 +264,9 @@ __device__ __forceinline__ void choose_experts(const ScoredRouter& r, const Lane
     if (!((kept >> bias.group0) & 1ull)) k0 = 0u;
     if (!((kept >> bias.group1) & 1ull)) k1 = 0u;
   }
+  // a barred logit comes last, whatever its bias for the choice
+  if (l0 == -INFINITY && k0) k0 = entry_key(-INFINITY, lane);
+  if (l1 == -INFINITY && k1) k1 = entry_key(-INFINITY, lane + 32);
   // The k largest: lane j keeps the j-th and its key.
   Entries rest(k0, k1, lane);
   uint32_t key = 0u;
@@ -375,9 +378,10 @@ __device__ __noinline__ void choose_exactly(const ScoredRouter& r, double l0, do
       double lm = fmax(v0 ? l0 : -INFINITY, v1 ? l1 : -INFINITY);
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) lm = fmax(lm, __shfl_xor_sync(0xffffffffu, lm, o));
+      lm = fmax(lm, -1e300);                       // (all barred: scores of 0)
       c0 = v0 ? exp(l0 - lm) : 0.0;
       c1 = v1 ? exp(l1 - lm) : 0.0;
-      const double den = r.select_bias ? warp_sum_f64(c0 + c1) : 1.0;
+      const double den = r.select_bias ? fmax(warp_sum_f64(c0 + c1), 1.0) : 1.0;
       c0 /= den;
       c1 /= den;
     }
@@ -428,6 +432,8 @@ __device__ __noinline__ void choose_exactly(const ScoredRouter& r, double l0, do
     if (!((eligible >> lane) & 1ull)) k0 = 0ull;
     if (!((eligible >> (lane + 32)) & 1ull)) k1 = 0ull;
   }
+  if (l0 == -INFINITY && k0) k0 = order_key(l0);   // barred
+  if (l1 == -INFINITY && k1) k1 = order_key(l1);
   slot0 = slot1 = -1;
 #pragma unroll 1
   for (int j = 0; j < r.k; ++j) {

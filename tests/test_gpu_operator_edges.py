@@ -83,3 +83,37 @@ def test_route_scored_wide_tokens_get_the_same_experts_in_every_batch(mote, d, E
     assert bool((long == want).all())
     assert torch.equal(mote.mote_route_scored(r, x)[0].cpu(), want)
     assert torch.equal(mote.mote_route_scored(r, x[5:6])[0].cpu(), want[5:6])
+
+
+@pytest.mark.parametrize("tokens", [1, 40, 2600])
+@pytest.mark.parametrize("scoring", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("n_groups,topk_groups", [(1, 1), (4, 3), (8, 8)])
+def test_route_scored_barred_logits_are_last_whatever_the_bias(mote, tokens, scoring, n_groups, topk_groups):
+    """A logit_bias of -inf bars an expert that select_bias favours too; where all are barred, the lower indices and weights of 0."""
+    E, d, k = 64, 512, 6
+    x = _randn(211, tokens, d).bfloat16()
+    x[-1] = 0.0
+    Wr = _randn(212, E, d) * 0.02
+    sb = _randn(213, E) * 0.02
+    lb = torch.zeros(E, device="cuda")
+    lb[1::3] = -float("inf")
+    sb[1::3] = 0.9
+    opt = dict(scoring=scoring, n_groups=n_groups, topk_groups=topk_groups)
+    idx, w, logits = mote.mote_route_scored(mote.MoteRouter(Wr, k, logit_bias=lb, select_bias=sb, **opt), x, want_logits=True)
+    assert bool((idx % 3 != 1).all()) and bool((w > 0.0).all())
+    assert bool((logits[:, 1::3] == -float("inf")).all())
+    ref = O.route_scored(_f64(x), _f64(Wr), k, logit_bias=_f64(lb), select_bias=_f64(sb), **opt)
+    assert np.array_equal(idx.cpu().numpy(), ref["idx"])
+    # four are left: the others follow, the lower index first, with weights of 0
+    lb[:] = -float("inf")
+    lb[[3, 17, 40, 63]] = 0.0
+    four = mote.mote_route_scored(mote.MoteRouter(Wr, k, logit_bias=lb, select_bias=sb, scoring=scoring), x)
+    assert bool((four[0][:, :4].sort(dim=1).values.cpu() == torch.tensor([3, 17, 40, 63])).all())
+    assert bool((four[0][:, 4:].cpu() == torch.tensor([0, 1])).all()) and bool((four[1][:, 4:] == 0.0).all())
+    # none is left
+    lb[:] = -float("inf")
+    for bias in (None, sb):
+        for renorm in (True, False):
+            idx, w, _ = mote.mote_route_scored(mote.MoteRouter(Wr, k, logit_bias=lb, select_bias=bias, renorm=renorm, **opt), x)
+            ref = O.route_scored(_f64(x[:1]), _f64(Wr), k, logit_bias=_f64(lb), select_bias=_f64(bias), **opt)
+            assert bool((idx.cpu() == torch.from_numpy(ref["idx"])).all()) and bool((w == 0.0).all())
