@@ -18,7 +18,7 @@
  *     anything is launched.  A failed launch maps to MOTE_ERR_CUDA.  No exceptions, no exit().
  *   - bf16 tensors are raw 16-bit patterns.  Matrices are row-major; a weight matrix is W[m, n]
  *     with n the reduction ("in") dimension, y = W x.
- *   - Non-finite inputs give undefined results.
+ *   - Non-finite inputs give undefined results where a call does not say otherwise.
  */
 #ifndef MOTE_H_
 #define MOTE_H_
@@ -385,7 +385,8 @@ mote_status_t mote_block_norm(const mote_block_norm_t* N, const void* y_bf16, in
  *
  *   out = act( w_scale[n] * sum_j x[t, j] W[n, j] + bias[n] ) + residual[t, n]
  *
- * fp32 accumulation and epilogue, one rounding to the output's type.
+ * fp32 accumulation and epilogue, one rounding to the output's type.  A value that is not finite goes through act as through
+ * its formula: NaN stays NaN, +inf stays +inf, -inf gives 0 with RELU and NaN with SILU and either GELU (-inf * 0).
  *   W         [N, K] bf16 (bits = 16 or 0), or the q of mote_rtn_quant with its scale (bits = 8 or 4)
  *   bias      [N] float or NULL;  act: MOTE_ACT_* (GELU with erf, GELU_TANH its tanh form)
  *   x_bf16    in  [T, K] bf16, row stride ldx elements (ldx >= K, ldx % 8 == 0)

@@ -28,6 +28,14 @@ __device__ __forceinline__ float rcp_fast(float x) {
   return y;
 }
 
+// The larger of z and 0; NaN stays NaN.
+__device__ __forceinline__ float relu_nan(float z) {
+  float y;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(z), "f"(0.0f));
+  return y;
+}
+constexpr float kGeluFlat = 16.0f;               // from here on gelu(z) = z in fp32, and for z = inf
+
 // Activations by a few instructions each (with expf, a division and erff the SiLU epilogue of a 4096 x 11008 product took longer than its
 // MMAs: 192 us instead of 128).  Errors are below 2^-21 of |z|.
 __device__ __forceinline__ float act_silu(float z) { return z * rcp_fast(1.0f + ex2_fast(-1.4426950408889634f * z)); }
@@ -38,19 +46,19 @@ __device__ __forceinline__ float act_gelu_tanh(float z) {
 }
 __device__ __forceinline__ float act_gelu(float z) {
   // erfc(x) = (a1 t + ... + a5 t^5) exp(-x^2), t = 1 / (1 + p x), x >= 0, to 1.5e-7 (Abramowitz and Stegun, 7.1.26);
-  // gelu(z) = max(z, 0) - |z| / 2 erfc(|z| / sqrt 2)
-  const float x = fabsf(z) * 0.70710678118654752f;
+  // gelu(z) = max(z, 0) - |z| / 2 erfc(|z| / sqrt 2); the second part is 0 long before kGeluFlat
+  const float mag = fabsf(fminf(z, kGeluFlat)), x = mag * 0.70710678118654752f;
   const float t = rcp_fast(fmaf(0.3275911f, x, 1.0f));
   float q = fmaf(1.061405429f, t, -1.453152027f);
   q = fmaf(q, t, 1.421413741f);
   q = fmaf(q, t, -0.284496736f);
   q = fmaf(q, t, 0.254829592f);
-  const float e = ex2_fast(-0.72134752044448170f * z * z);               // exp(-z^2 / 2)
-  return fmaf(-0.5f * fabsf(z), q * t * e, fmaxf(z, 0.0f));
+  const float e = ex2_fast(-0.72134752044448170f * mag * mag);           // exp(-z^2 / 2)
+  return fmaf(-0.5f * mag, q * t * e, relu_nan(z));
 }
 __device__ __forceinline__ float apply_act(float z, int act) {
   switch (act) {
-    case MOTE_ACT_RELU: return fmaxf(z, 0.0f);
+    case MOTE_ACT_RELU: return relu_nan(z);
     case MOTE_ACT_SILU: return act_silu(z);
     case MOTE_ACT_GELU: return act_gelu(z);
     case MOTE_ACT_GELU_TANH: return act_gelu_tanh(z);
@@ -77,7 +85,12 @@ __device__ __forceinline__ uint64_t rcp_pair(uint64_t v) {
 __device__ __forceinline__ uint64_t max0_pair(uint64_t v) {
   float a, b;
   unpack_f32x2(v, a, b);
-  return f32x2(fmaxf(a, 0.0f), fmaxf(b, 0.0f));
+  return f32x2(relu_nan(a), relu_nan(b));
+}
+__device__ __forceinline__ uint64_t flat_magnitude_pair(uint64_t v) {            // |min(v, kGeluFlat)|
+  float a, b;
+  unpack_f32x2(v, a, b);
+  return f32x2(fabsf(fminf(a, kGeluFlat)), fabsf(fminf(b, kGeluFlat)));
 }
 // z / (1 + 2^m)
 __device__ __forceinline__ uint64_t gated_pair(uint64_t z, uint64_t m) {
@@ -99,13 +112,13 @@ __device__ __forceinline__ void apply_act16(uint64_t (&z)[8], int act) {
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {                // act_gelu
-      const uint64_t mag = z[j] & 0x7FFFFFFF7FFFFFFFull;
+      const uint64_t mag = flat_magnitude_pair(z[j]);
       const uint64_t t = rcp_pair(fma2(mag, both(0.3275911f * 0.70710678118654752f), both(1.0f)));
       uint64_t q = fma2(both(1.061405429f), t, both(-1.453152027f));
       q = fma2(q, t, both(1.421413741f));
       q = fma2(q, t, both(-0.284496736f));
       q = fma2(q, t, both(0.254829592f));
-      const uint64_t e = ex2_pair(mul_f32x2(mul_f32x2(z[j], both(-0.72134752044448170f)), z[j]));
+      const uint64_t e = ex2_pair(mul_f32x2(mul_f32x2(mag, both(-0.72134752044448170f)), mag));
       z[j] = fma2(mul_f32x2(mag, both(-0.5f)), mul_f32x2(mul_f32x2(q, t), e), max0_pair(z[j]));
     }
   }

@@ -117,3 +117,29 @@ def test_route_scored_barred_logits_are_last_whatever_the_bias(mote, tokens, sco
             idx, w, _ = mote.mote_route_scored(mote.MoteRouter(Wr, k, logit_bias=lb, select_bias=bias, renorm=renorm, **opt), x)
             ref = O.route_scored(_f64(x[:1]), _f64(Wr), k, logit_bias=_f64(lb), select_bias=_f64(bias), **opt)
             assert bool((idx.cpu() == torch.from_numpy(ref["idx"])).all()) and bool((w == 0.0).all())
+
+
+# ------------------------------------------------------------------------------------------------ projections
+ACTS = ["none", "relu", "silu", "gelu", "gelu_tanh"]
+
+
+@pytest.mark.parametrize("out_dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T,N", [(1, 72), (9, 71), (40, 72), (200, 72), (300, 71), (1500, 264)])
+@pytest.mark.parametrize("act", ACTS)
+def test_linear_values_that_are_not_finite(mote, act, T, N, out_dtype):
+    """NaN and infinities before the activation (from a bias, from a token, from a weight) come out as the formula gives them."""
+    K, inf = 256, float("inf")
+    x, W, b = _randn(221, T, K).bfloat16(), (_randn(222, N, K) * 0.05).bfloat16(), _randn(223, N)
+    b[3], b[17], b[40] = inf, -inf, float("nan")
+    got = mote.mote_linear(mote.MoteLinear(W, bias=b, act=act), x, out_dtype=out_dtype).double().cpu().numpy()
+    with np.errstate(invalid="ignore"):
+        want = O.activation(np.array([inf, -inf, np.nan]), act)
+    assert np.array_equal(got[:, [3, 17, 40]], np.broadcast_to(want, (T, 3)), equal_nan=True), got[0, [3, 17, 40]]
+    rest = np.delete(got, [3, 17, 40], axis=1)
+    assert np.isfinite(rest).all()
+    # a NaN of a token reaches its whole row and no other, one of a weight its column
+    b = torch.zeros(N, device="cuda")
+    x[T // 2, 7] = float("nan")
+    W[5, 100] = float("nan")
+    got = mote.mote_linear(mote.MoteLinear(W, bias=b, act=act), x, out_dtype=out_dtype).isnan()
+    assert bool(got[T // 2].all()) and bool(got[:, 5].all()) and int(got.sum()) == N + T - 1
