@@ -143,3 +143,33 @@ def test_linear_values_that_are_not_finite(mote, act, T, N, out_dtype):
     W[5, 100] = float("nan")
     got = mote.mote_linear(mote.MoteLinear(W, bias=b, act=act), x, out_dtype=out_dtype).isnan()
     assert bool(got[T // 2].all()) and bool(got[:, 5].all()) and int(got.sum()) == N + T - 1
+
+
+@pytest.mark.parametrize("T,bits", [(7, 16), (16, 8), (400, 16), (1000, 4)])
+@pytest.mark.parametrize("act", ACTS)
+def test_linear_activations_relative_to_their_own_size(mote, act, T, bits):
+    """Every product but one is zero, so z is known exactly: the activation's error relative to its value, in the tails too.
+    Special-function results are off by 2^-22, the fit of the GELU's tail by 2^-20.9; a rounding (2^-24, up to seven of them with those of z
+    and the constants) of an exponent a moves e^a by its part of a: |z|, twice the tanh's argument, or z^2 / 2."""
+    from math import erfc
+    K = 16
+    z = torch.linspace(-13.0, 13.0, T * K, dtype=torch.float64).view(T, K)
+    z[0, :4] = torch.tensor([0.0, 1e-3, -1e-3, -1e-20])
+    x = z.to("cuda").bfloat16()
+    if bits == 16:
+        lin = mote.MoteLinear(torch.eye(K, device="cuda").bfloat16(), act=act)
+    else:
+        lin = mote.MoteLinear.quantized(torch.eye(K, device="cuda"), bits, act=act)
+    z = _f64(x) * (1.0 if bits == 16 else lin.tensors["scale"].double().cpu().numpy() * (127 if bits == 8 else 7))
+    u = np.sqrt(2.0 / np.pi) * (z + 0.044715 * z ** 3)
+    if act == "gelu":
+        want = z * 0.5 * np.vectorize(erfc)(-z / np.sqrt(2.0))
+    elif act == "gelu_tanh":
+        want = z / (1.0 + np.exp(-2.0 * u))
+    else:
+        want = O.activation(z, act)
+    exponent = {"none": 0.0 * z, "relu": 0.0 * z, "silu": np.abs(z), "gelu": z * z / 2.0, "gelu_tanh": 2.0 * np.abs(u)}[act]
+    got = _f64(mote.mote_linear(lin, x, out_dtype=torch.float32))
+    seen = (np.abs(want) > 1e-35) | (want == 0.0)
+    assert np.all(np.abs(got - want)[seen] <= ((2.0 ** -19 + exponent * 2.0 ** -21) * np.abs(want))[seen])
+    assert np.all(np.abs(got - want)[~seen] <= 1e-35)
