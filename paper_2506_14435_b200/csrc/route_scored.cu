@@ -128,7 +128,7 @@ struct Doubt {
   uint64_t chosen;                                 // the fp32 choice, six bits each
 };
 
-// 1 / x and e^x of the special-function unit: a few 2^-23 (and |x| 2^-24) off, which the bounds have room for.
+// 1 / x of the special-function unit: 2^-23 off, as the library's e^x is (2 ulp; __expf, whose error grows with |x|, is no faster here).
 __device__ __forceinline__ float rcp_approx(float x) {
   float y;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -176,12 +176,12 @@ __device__ __forceinline__ void choose_experts(const ScoredRouter& r, const Lane
   float smax = 1.0f;
   d.l_max = d.inv_den = d.den_rel = 0.0f;
   if (r.sigmoid) {
-    p0 = rcp_approx(1.0f + __expf(-l0));
-    p1 = rcp_approx(1.0f + __expf(-l1));
+    p0 = rcp_approx(1.0f + expf(-l0));
+    p1 = rcp_approx(1.0f + expf(-l1));
   } else {
     const float lm = fmaxf(warp_max(fmaxf(v0 ? l0 : -INFINITY, v1 ? l1 : -INFINITY)), -3.4e38f);      // (all barred: scores of 0)
-    p0 = v0 ? __expf(l0 - lm) : 0.0f;
-    p1 = v1 ? __expf(l1 - lm) : 0.0f;
+    p0 = v0 ? expf(l0 - lm) : 0.0f;
+    p1 = v1 ? expf(l1 - lm) : 0.0f;
     smax = rcp_approx(fmaxf(warp_sum(p0 + p1), 1.0f));             // (1 is the largest one's part; less where all are barred)
     d.l_max = lm;
     d.inv_den = smax;
@@ -190,7 +190,7 @@ __device__ __forceinline__ void choose_experts(const ScoredRouter& r, const Lane
     p1 *= smax;
   }
   const float c0 = (by_logit ? l0 : p0) + bias.s0, c1 = (by_logit ? l1 : p1) + bias.s1;
-  // bound on the error of c: of the logit through the score's slope, of expf and the division, of adding the bias
+  // bound on the error of c: of the logit through the score's slope, of expf and the reciprocal, of adding the bias
   float tau = (by_logit ? delta : r.sigmoid ? 0.25f * delta + 4.8e-7f : delta < 0.5f ? smax * (2.0f * delta * (1.0f + 2.0f * delta) + 4e-6f) : 1e30f) + 1.2e-7f * bias.select_max;
   uint32_t k0 = v0 ? entry_key(c0, lane) : 0u, k1 = v1 ? entry_key(c1, lane + 32) : 0u, best;
   d.full = 0;

@@ -119,6 +119,26 @@ def test_route_scored_barred_logits_are_last_whatever_the_bias(mote, tokens, sco
             assert bool((idx.cpu() == torch.from_numpy(ref["idx"])).all()) and bool((w == 0.0).all())
 
 
+@pytest.mark.parametrize("tokens", [9, 3000])
+@pytest.mark.parametrize("renorm", [True, False])
+@pytest.mark.parametrize("scoring", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("spread", [0.5, 8.0, 25.0])
+def test_route_scored_weights_of_exact_logits(mote, scoring, spread, renorm, tokens):
+    """Tokens with one channel of 1: the logits are the router's entries, so the weights' own arithmetic is seen.  In units of 2^-24: e^x 4, its
+    argument's rounding |x|, seven additions, reciprocals and products of 2 and 1 each, twice with renorm: 32 and |x| at most."""
+    E, d, k = 16, 1024, 8
+    x = torch.zeros(tokens, d, device="cuda")
+    x[torch.arange(tokens), torch.arange(tokens) % d] = 1.0
+    Wr = _randn(231, E, d) * spread
+    idx, w, logits = mote.mote_route_scored(mote.MoteRouter(Wr, k, scoring=scoring, renorm=renorm, scale=2.5), x.bfloat16(), want_logits=True)
+    l = Wr.T[torch.arange(tokens) % d]
+    assert torch.equal(logits, l)
+    ref = O.route_scored(_f64(x), _f64(Wr), k, scoring=scoring, renorm=renorm, scale=2.5)
+    assert np.array_equal(idx.cpu().numpy(), ref["idx"])
+    far = _f64(l.max(dim=1, keepdim=True).values - l.gather(1, idx.long())) if scoring == "softmax" else 0.0
+    assert np.all(np.abs(_f64(w) - ref["w"]) <= (32.0 + far) * 2.0 ** -24 * ref["w"] + 1e-37)
+
+
 # ------------------------------------------------------------------------------------------------ projections
 ACTS = ["none", "relu", "silu", "gelu", "gelu_tanh"]
 
