@@ -386,7 +386,10 @@ mote_status_t mote_block_norm(const mote_block_norm_t* N, const void* y_bf16, in
  *
  *   out = act( w_scale[n] * sum_j x[t, j] W[n, j] + bias[n] ) + residual[t, n]
  *
- * fp32 accumulation and epilogue, one rounding to the output's type.  A value that is not finite goes through act as through
+ * fp32 accumulation and epilogue, one rounding to the output's type.  The accumulators are the tensor cores', which cut off
+ * where they add up instead of rounding: a sum is off by at most 0.66 K 2^-24 of its largest partial sum.  Measured, relative to
+ * the whole: terms of one sign 0.9e-6 (K = 2048), 3e-6 (11008), 35e-6 (65536), random signs 0.5e-6, 1.4e-6, 9e-6 of the output's norm; up to
+ * 16 tokens a third of that.  It shows with fp32 outputs only.  A value that is not finite goes through act as through
  * its formula: NaN stays NaN, +inf stays +inf, -inf gives 0 with RELU and NaN with SILU and either GELU (-inf * 0).
  *   W         [N, K] bf16 (bits = 16 or 0), or the q of mote_rtn_quant with its scale (bits = 8 or 4)
  *   bias      [N] float or NULL;  act: MOTE_ACT_* (GELU with erf, GELU_TANH its tanh form)

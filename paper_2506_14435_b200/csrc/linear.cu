@@ -3,7 +3,9 @@
 //   out = act( scale_n * (x W^T) + bias ) [+ residual]
 //
 // W [N, K] is bf16, or the RTN codes of mote_rtn_quant (INT8 / INT4) with one scale per row; fp32 accumulation, one rounding
-// to the output's type.
+// to the output's type.  The whole of K (a warp's or a cluster rank's part of it) is left to the tensor cores' accumulators, which cut off what
+// lies 25 bits below the largest addend: 3e-6 of a sum of one sign at K = 11008 (mote.h), below a thousandth of a bf16 output's rounding.
+// (The router, whose choice hangs on the last bits, takes its sums out every few steps.)
 //
 // For few tokens the product is a weight stream, bound by HBM and, at these sizes, by how much is in flight: a CTA owns 16 rows
 // of W, its warps share K, and asynchronous copies bring weights and tokens to rings in shared memory, from where they feed warp-level

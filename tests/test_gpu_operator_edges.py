@@ -193,3 +193,30 @@ def test_linear_activations_relative_to_their_own_size(mote, act, T, bits):
     seen = (np.abs(want) > 1e-35) | (want == 0.0)
     assert np.all(np.abs(got - want)[seen] <= ((2.0 ** -19 + exponent * 2.0 ** -21) * np.abs(want))[seen])
     assert np.all(np.abs(got - want)[~seen] <= 1e-35)
+
+
+@pytest.mark.parametrize("T,N,K", [(1, 40, 4096), (8, 33, 11008), (16, 48, 2048), (24, 40, 4096), (64, 24, 2048), (130, 24, 2048), (40, 16, 11008)])
+@pytest.mark.parametrize("bits", [16, 8, 4])
+@pytest.mark.parametrize("sign", ["random", "one"])
+def test_linear_sums_in_32_bits(mote, T, N, K, bits, sign):
+    """fp32 outputs against a bound that a partial sum rounded to fewer bits breaks.  A tensor-core instruction cuts its 16 products and the
+    sum so far off 25 bits below the largest, and the result to 24: 10.5 units of 2^-24 of the largest magnitude there is.  That is a
+    partial sum (a difference of two prefixes) or what one step of up to 64 products comes to.  20 units for the meeting of parts."""
+    x, W = _randn(251, T, K), _randn(252, N, K) * 0.05
+    if sign == "one":
+        x, W = x.abs(), W.abs()
+    x, b = x.bfloat16(), _randn(253, N)
+    lin = mote.MoteLinear(W.bfloat16(), bias=b) if bits == 16 else mote.MoteLinear.quantized(W, bits, bias=b)
+    if bits == 16:
+        Wd, scale = _f64(W.bfloat16()), np.ones(N)
+    else:
+        q, _ = O.rtn_quantize(W.cpu().numpy(), bits)
+        Wd, scale = q.astype(np.float64), lin.tensors["scale"].double().cpu().numpy()
+    got = _f64(mote.mote_linear(lin, x, out_dtype=torch.float32))
+    p = torch.from_numpy(_f64(x)).cuda()[:, None, :] * torch.from_numpy(Wd).cuda()[None]                # [T, N, K]
+    prefix = p.view(T, N, K // 16, 16).sum(dim=3).cumsum(dim=2).abs().amax(dim=2)
+    step = p.abs().view(T, N, K // 64, 64).sum(dim=3).amax(dim=2)
+    largest = (2.0 * prefix + step).cpu().numpy() * scale
+    want = p.sum(dim=2).cpu().numpy() * scale + _f64(b)
+    tol = (10.5 * K / 16 + 20.0) * 2.0 ** -24 * largest + 4.0 * 2.0 ** -24 * np.abs(want - _f64(b)) + 2.0 ** -24 * np.abs(want)
+    assert np.all(np.abs(got - want) <= tol), float((np.abs(got - want) / tol).max())
