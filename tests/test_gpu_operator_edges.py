@@ -5,6 +5,8 @@ import pytest
 import torch
 
 from oracle import mote_oracle as O
+from parity_utils import REL_FRO_TOL, bf16_bits, bf16_tensor
+from workloads import synth
 
 pytestmark = pytest.mark.gpu
 
@@ -139,6 +141,30 @@ def test_route_scored_weights_of_exact_logits(mote, scoring, spread, renorm, tok
     assert np.all(np.abs(_f64(w) - ref["w"]) <= (32.0 + far) * 2.0 ** -24 * ref["w"] + 1e-37)
 
 
+@pytest.mark.parametrize("tokens,d,E", [(1, 2048, 64), (50, 896, 60), (700, 5000, 16), (1200, 2048, 64), (2003, 5000, 64), (300, 32768, 64)])
+@pytest.mark.parametrize("kind", ["normal", "outliers", "positive"])
+@pytest.mark.parametrize("w_dtype", [torch.float32, torch.bfloat16])
+def test_route_scored_logits_within_the_bound_the_choice_relies_on(mote, tokens, d, E, kind, w_dtype):
+    """A logit: 27 units of 2^-24 |x| |w|, and a weight what that and 32 units of its own arithmetic make of it."""
+    x, Wr = _randn(241, tokens, d), _randn(242, E, d) * 0.02
+    if kind == "outliers":
+        x[:, ::97] *= 20.0
+    elif kind == "positive":
+        x, Wr = x.abs(), Wr.abs()
+    x, Wr = x.bfloat16(), Wr.to(w_dtype)
+    lb = _randn(243, E)
+    for scoring in ("softmax", "sigmoid"):
+        idx, w, logits = mote.mote_route_scored(mote.MoteRouter(Wr, 4, scoring=scoring, logit_bias=lb), x, want_logits=True)
+        ref = O.route_scored(_f64(x), _f64(Wr), 4, scoring=scoring, logit_bias=_f64(lb))
+        norms = np.linalg.norm(_f64(x), axis=1)[:, None] * np.linalg.norm(_f64(Wr), axis=1)[None]
+        err = 27.0 * 2.0 ** -24 * norms + 2.0 ** -23 * np.abs(_f64(lb))
+        assert np.all(np.abs(_f64(logits) - ref["logits"]) <= err)
+        assert np.array_equal(idx.cpu().numpy(), ref["idx"])
+        # a score moves by its logit's error and its denominator's, a renormalised one by the others' too
+        rel = np.expm1(2.0 * err.max(axis=1, keepdims=True)) + (32.0 + np.ptp(ref["logits"], axis=1, keepdims=True)) * 2.0 ** -24
+        assert np.all(np.abs(_f64(w) - ref["w"]) <= rel * ref["w"])
+
+
 # ------------------------------------------------------------------------------------------------ projections
 ACTS = ["none", "relu", "silu", "gelu", "gelu_tanh"]
 
@@ -220,3 +246,67 @@ def test_linear_sums_in_32_bits(mote, T, N, K, bits, sign):
     want = p.sum(dim=2).cpu().numpy() * scale + _f64(b)
     tol = (10.5 * K / 16 + 20.0) * 2.0 ** -24 * largest + 4.0 * 2.0 ** -24 * np.abs(want - _f64(b)) + 2.0 ** -24 * np.abs(want)
     assert np.all(np.abs(got - want) <= tol), float((np.abs(got - want) / tol).max())
+
+
+# ------------------------------------------------------------------------------------------------ the layer with a scored router
+SIMT, TENSOR, STREAM, AUTO = 1, 2, 3, 0
+
+
+@pytest.mark.parametrize("bits", [16, 8, 4])
+@pytest.mark.parametrize("d,f,E,k,T,path,opt", [
+    (64, 112, 5, 5, 33, SIMT, dict()),                               # k = E
+    (256, 512, 4, 2, 300, SIMT, dict(renorm=False)),
+    (128, 128, 2, 1, 1, TENSOR, dict(scoring="sigmoid")),
+    (384, 640, 3, 3, 515, TENSOR, dict()),
+    (128, 256, 64, 8, 200, TENSOR, dict(scoring="sigmoid", n_groups=8, topk_groups=4, scale=2.5, sb=True)),
+    (256, 128, 16, 4, 1000, TENSOR, dict(n_groups=4, topk_groups=3, lb=True, w=torch.bfloat16)),
+    (896, 4864, 4, 2, 160, TENSOR, dict(lb=True)),
+    (256, 512, 4, 2, 900, TENSOR, dict(scoring="sigmoid", renorm=False)),
+    (128, 192, 2, 1, 1, STREAM, dict()),
+    (896, 4864, 4, 2, 2, STREAM, dict(scoring="sigmoid", sb=True)),
+    (896, 4864, 4, 2, 17, STREAM, dict(lb=True, bar=1)),             # an expert without tokens
+    (512, 1024, 8, 2, 13, STREAM, dict(n_groups=4, topk_groups=2, scale=0.5)),
+    (128, 256, 64, 8, 37, STREAM, dict(scoring="sigmoid", n_groups=8, topk_groups=2, sb=True, w=torch.bfloat16)),
+    (256, 512, 4, 2, 64, STREAM, dict(lb=True, bar=2)),
+    (128, 256, 16, 2, 12800, AUTO, dict(scoring="sigmoid", n_groups=4, topk_groups=2, sb=True)),
+])
+def test_moe_forward_scored_over_shapes(mote, d, f, E, k, T, path, opt, bits):
+    o = dict(opt)
+    wl = synth.custom("scored", d, f, E, k, T, 9000 + d + f + T, w_std=0.08)
+    master = synth.master_layer(wl)
+    layer, layer_or = mote.MoteLayer.from_master(master, path=path), O.build_layer(master)
+    if bits != 16:
+        layer, layer_or = layer.quantize_shared(bits), O.quantize_shared(layer_or, bits)
+    Wr = (_randn(261, E, d) * 0.1).to(o.pop("w", torch.float32))
+    lb = _randn(262, E) * 0.3 if o.pop("lb", False) else None
+    if "bar" in o:
+        lb[o.pop("bar")] = -float("inf")
+    sb = _randn(263, E) * 0.05 if o.pop("sb", False) else None
+    router = mote.MoteRouter(Wr, k, logit_bias=lb, select_bias=sb, **o)
+    x_bits = synth.tokens(wl)
+    x, res = bf16_tensor(x_bits), _randn(264, T, d).bfloat16()
+    taps = layer.alloc_taps(T)
+    out = mote.mote_moe_forward_scored(layer, router, x, residual=res, taps=taps)
+    assert mote.lib.mote_device_status(layer._ws.data_ptr(), None) == 0
+    some = np.arange(T) if T <= 1000 else np.arange(0, T, 41)       # (the oracle's layer token by token)
+    route = O.route_scored(_f64(x), _f64(Wr), k, logit_bias=_f64(lb), select_bias=_f64(sb), **o)
+    assert np.array_equal(taps["topk_idx"].cpu().numpy(), route["idx"])
+    part = dict(logits=route["logits"][some], idx=route["idx"][some], w=route["w"][some], near_tie=route["near_tie"][some])
+    ref = O.moe_forward(layer_or, x_bits[some], residual_bf16=bf16_bits(res)[some], route=part)
+    if T == len(some):
+        for name in ("offsets", "perm", "qx", "beta_x", "acc_gate", "acc_up", "qh", "beta_h", "acc_down"):
+            assert np.array_equal(taps[name].cpu().numpy(), ref[name]), name
+    got = O.bf16_to_f32(bf16_bits(out)[some]).astype(np.float64)
+    assert np.linalg.norm(got - ref["out"]) / np.linalg.norm(ref["out"]) <= REL_FRO_TOL
+    # captured, for other tokens; out in the residual's place
+    x2 = bf16_tensor(synth.tokens(wl, stream=1))
+    want = mote.mote_moe_forward_scored(layer, router, x2, residual=res)
+    graph = torch.cuda.CUDAGraph()
+    place = res.clone()
+    with torch.cuda.graph(graph):
+        mote.mote_moe_forward_scored(layer, router, x, residual=place, out=place)
+    x.copy_(x2)
+    place.copy_(res)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(place, want)
