@@ -4,6 +4,7 @@ memory and streams."""
 from __future__ import annotations
 
 import ctypes as C
+import importlib
 import os
 
 import torch
@@ -14,11 +15,25 @@ if not os.path.exists(_LIB_PATH):
     raise ImportError(f"{_LIB_PATH} is missing: build it with `python -m paper_2506_14435_b200.build`; "
                       "there is no fallback path")
 lib = C.CDLL(_LIB_PATH)
-try:
-    from . import _calls
-except ImportError as e:
-    raise ImportError("paper_2506_14435_b200/_calls.so is missing or was built for another torch: build it with "
-                      "`python -m paper_2506_14435_b200.build`") from e
+
+
+class _Calls:
+    """_calls.so, imported when one of the calls that go through it is made first: it fits one version of torch only, and all others do
+    without it."""
+
+    def __getattr__(self, name):
+        global _calls
+        if name.startswith("__"):
+            raise AttributeError(name)
+        try:
+            _calls = importlib.import_module("._calls", __package__)
+        except ImportError as e:
+            raise ImportError("paper_2506_14435_b200/_calls.so is missing or was built for another torch: build it with "
+                              "`python -m paper_2506_14435_b200.build`; there is no fallback path") from e
+        return getattr(_calls, name)
+
+
+_calls = _Calls()
 
 PATH_AUTO, PATH_SIMT, PATH_TENSOR, PATH_STREAM = 0, 1, 2, 3
 DTYPE_F32, DTYPE_BF16 = 0, 1

@@ -1,0 +1,46 @@
+"""The binding of the operators around the experts, on the host: what it needs, what it refuses, how its extension module is built."""
+import os
+import subprocess
+import sys
+
+import pytest
+import torch
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def b():
+    from paper_2506_14435_b200 import build
+    build.build()
+    from paper_2506_14435_b200 import binding
+    return binding
+
+
+def test_only_the_calls_that_go_through_the_extension_module_need_it(b):
+    """As with another torch than the one it was built for, or before it is built."""
+    code = """
+import importlib.abc, sys
+class Block(importlib.abc.MetaPathFinder):
+    def find_spec(self, name, path, target=None):
+        if name == "paper_2506_14435_b200._calls":
+            raise ImportError("undefined symbol")
+sys.meta_path.insert(0, Block())
+import torch
+import paper_2506_14435_b200 as mote
+assert mote.lib.mote_route_scored(None, None, 0, 0, None, None, None, None) == 1
+assert mote.lib.mote_rms_norm(None, 0, 64, 1e-6, None, None) == 0
+for name in mote.__all__:
+    getattr(mote, name)
+norm = mote.MoteBlockNorm(64)
+for _ in range(2):
+    try:
+        mote.mote_block_norm(norm, torch.zeros(3, 64, dtype=torch.bfloat16))
+    except ImportError as e:
+        assert "_calls.so" in str(e) and "paper_2506_14435_b200.build" in str(e)
+    else:
+        raise AssertionError("no error")
+print("done")
+"""
+    r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and r.stdout.strip() == "done", r.stderr
