@@ -66,6 +66,26 @@ def _compile_calls() -> str:
     return obj
 
 
+def _link_calls(obj: str) -> None:
+    """The extension module from its object file.  Objects of several torch versions can lie side by side: what the module was linked from is
+    noted, since an older object may be another version's."""
+    note, source = os.path.join(OBJ, "_calls.linked"), f"{obj} {os.path.getmtime(obj)}"
+    if os.path.exists(CALLS) and os.path.exists(note):
+        with open(note) as f:
+            if f.read() == source:
+                return
+    import torch
+    libs = os.path.join(os.path.dirname(torch.__file__), "lib")
+    cmd = ["g++", "-shared", "-o", CALLS, obj, "-L" + PKG, "-l:libmote.so", "-Wl,-rpath,$ORIGIN", "-L" + libs,
+           "-ltorch_python", "-ltorch_cuda", "-ltorch_cpu", "-lc10_cuda", "-lc10"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode:
+        sys.stderr.write(r.stdout + r.stderr)
+        raise RuntimeError("link of _calls.so failed")
+    with open(note, "w") as f:
+        f.write(source)
+
+
 def build(verbose: bool = False) -> str:
     os.makedirs(OBJ, exist_ok=True)
     with ThreadPoolExecutor(max_workers=8) as ex:
@@ -77,16 +97,7 @@ def build(verbose: bool = False) -> str:
         if r.returncode:
             sys.stderr.write(r.stdout + r.stderr)
             raise RuntimeError("link failed")
-    calls = calls.result()
-    if not os.path.exists(CALLS) or os.path.getmtime(CALLS) < os.path.getmtime(calls):
-        import torch
-        libs = os.path.join(os.path.dirname(torch.__file__), "lib")
-        cmd = ["g++", "-shared", "-o", CALLS, calls, "-L" + PKG, "-l:libmote.so", "-Wl,-rpath,$ORIGIN", "-L" + libs,
-               "-ltorch_python", "-ltorch_cuda", "-ltorch_cpu", "-lc10_cuda", "-lc10"]
-        r = subprocess.run(cmd, capture_output=True, text=True)
-        if r.returncode:
-            sys.stderr.write(r.stdout + r.stderr)
-            raise RuntimeError("link of _calls.so failed")
+    _link_calls(calls.result())
     return LIB
 
 

@@ -44,3 +44,37 @@ print("done")
 """
     r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and r.stdout.strip() == "done", r.stderr
+
+
+def test_the_extension_module_is_linked_again_for_another_torch(b, monkeypatch, tmp_path):
+    """Objects of two torch versions lie side by side: going back to the first one links it again, although it is older than the library."""
+    from paper_2506_14435_b200 import build
+    linked, calls = [], tmp_path / "_calls.so"
+
+    class Done:
+        returncode, stdout, stderr = 0, "", ""
+
+    def run(cmd, **kw):
+        linked.append([c for c in cmd if c.endswith(".o")])
+        calls.write_text(str(linked[-1]))
+        return Done
+
+    monkeypatch.setattr(build, "CALLS", str(calls))
+    monkeypatch.setattr(build, "OBJ", str(tmp_path))
+    monkeypatch.setattr(build, "LIB", str(tmp_path / "libmote.so"))
+    monkeypatch.setattr(build, "_sources", lambda: [])
+    monkeypatch.setattr(build.subprocess, "run", run)
+    (tmp_path / "libmote.so").write_text("")
+    a, other = tmp_path / "torch_calls-A.o", tmp_path / "torch_calls-B.o"
+    a.write_text("")
+    other.write_text("")
+    os.utime(a, (1000, 1000))
+    os.utime(other, (2000, 2000))
+    for obj in (a, a, other, other, a, a):
+        monkeypatch.setattr(build, "_compile_calls", lambda obj=obj: str(obj))
+        build.build()
+        assert calls.read_text() == str([str(obj)])
+    assert linked == [[str(a)], [str(other)], [str(a)]]
+    os.utime(a, (3000, 3000))                              # compiled anew
+    build.build()
+    assert len(linked) == 4
