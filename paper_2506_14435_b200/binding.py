@@ -516,6 +516,8 @@ def mote_moe_forward_scored(layer: MoteLayer, router: MoteRouter, x: torch.Tenso
     for t, name in ((x, "x"), (residual, "residual"), (out, "out")):
         if t is not None and (t.dtype is not torch.bfloat16 or t.dim() != 2 or tuple(t.shape) != (x.shape[0], layer.d)):
             raise ValueError(f"{name}: expected bfloat16 [T, {layer.d}]")
+        if t is not None and t.requires_grad and torch.is_grad_enabled():
+            raise ValueError(f"{name}: requires grad, and there is no backward pass; call under torch.no_grad() or with a detached tensor")
     _need_cuda(x, residual, out)
     _here(router.device)
     if any(t is not None and t.get_device() != router.device for t in (x, residual, out, layer.tensors["Wr"])):

@@ -7,6 +7,7 @@
 #include <Python.h>
 #include <ATen/ATen.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/core/GradMode.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Dtype.h>
@@ -21,7 +22,10 @@ struct Refused { std::string why; };
 
 const at::Tensor& tensor(PyObject* o, const char* name) {
   if (!THPVariable_Check(o)) throw Refused{std::string(name) + ": expected a tensor"};
-  return THPVariable_Unpack(o);
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (t.requires_grad() && c10::GradMode::is_enabled())        // its gradient would be lost without a word
+    throw Refused{std::string(name) + ": requires grad, and there is no backward pass; call under torch.no_grad() or with a detached tensor"};
+  return t;
 }
 
 // the library works on the current device and stream

@@ -310,3 +310,23 @@ def test_moe_forward_scored_over_shapes(mote, d, f, E, k, T, path, opt, bits):
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(place, want)
+
+
+def test_operators_on_tensors_that_require_grad(mote):
+    d = 64
+    x = _randn(271, 5, d).bfloat16().requires_grad_()
+    res = _randn(272, 5, d).bfloat16().requires_grad_()
+    gate = _randn(273, 5, 1).requires_grad_()
+    lin, norm, router = mote.MoteLinear((_randn(274, d, d)).bfloat16()), mote.MoteBlockNorm(d), mote.MoteRouter(_randn(275, 8, d), 2)
+    plain = x.detach()
+    for call in (lambda: mote.mote_linear(lin, x), lambda: mote.mote_linear(lin, plain, residual=res), lambda: mote.mote_block_norm(norm, x),
+                 lambda: mote.mote_block_norm(norm, plain, res), lambda: mote.mote_block_norm(norm, plain, gate=gate),
+                 lambda: mote.mote_route_scored(router, x)):
+        with pytest.raises(ValueError, match="requires grad"):
+            call()
+        with torch.no_grad():
+            call()
+        with torch.inference_mode():
+            call()
+    with torch.no_grad():
+        assert torch.equal(mote.mote_linear(lin, x, residual=res), mote.mote_linear(lin, plain, residual=res.detach()))

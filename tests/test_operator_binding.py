@@ -78,3 +78,28 @@ def test_the_extension_module_is_linked_again_for_another_torch(b, monkeypatch, 
     os.utime(a, (3000, 3000))                              # compiled anew
     build.build()
     assert len(linked) == 4
+
+
+def test_tensors_that_require_grad_are_refused_where_grad_is_recorded(b):
+    """The operators have no backward pass: a gradient would be lost without a word."""
+    x = torch.zeros(3, 64, dtype=torch.bfloat16, requires_grad=True)
+    plain = torch.zeros(3, 64, dtype=torch.bfloat16)
+    norm = b.MoteBlockNorm(64)
+
+    class Router:                                                  # (nothing of them is read before the tensors)
+        device, _address = -1, 0
+
+    class Linear:
+        device, _address, _ws_T, _ws_address, _ws_bytes = -1, 0, 3, 0, 0
+
+    class Layer:
+        d = 64
+
+    calls = [lambda t: b.mote_block_norm(norm, t), lambda t: b.mote_route_scored(Router, t), lambda t: b.mote_linear(Linear, t),
+             lambda t: b.mote_moe_forward_scored(Layer, Router, t), lambda t: b.mote_moe_forward_scored(Layer, Router, plain, residual=t)]
+    for call in calls:
+        with pytest.raises(ValueError, match="requires grad"):
+            call(x)
+        with torch.no_grad(), pytest.raises(Exception) as e:       # not on a GPU
+            call(x)
+        assert "requires grad" not in str(e.value)
