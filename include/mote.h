@@ -361,7 +361,8 @@ mote_status_t mote_rms_norm(const void* x_bf16, int64_t T, int64_t d, float eps,
  *   y        in  [T, d] bf16, row stride ldy elements;  residual in [T, d] of res_dtype, row stride ldr elements, or NULL
  *            (zeros).  Strides >= d, rows on 16-byte boundaries.
  *   res_out  out [T, d] contiguous of res_dtype, or NULL;  normed_out out [T, d] bf16 contiguous, or NULL; not both NULL
- * An output may take the place of an input of the same element size and layout; any other overlap of the ranges is refused.
+ * An output may take the place of y or residual with the same element size and layout; any other overlap with an input, a gain or
+ * the other output is refused.
  * All pointers 16-B aligned but for a gate with gate_cols = 1 (its element's size).
  * T = 0 is a no-op.  Errors: T > 2^24, d % 8 != 0, d > 32768, eps < 0, gate_cols not 0, 1 or d, gate_tokens < 0, overlap -> ERR_SHAPE;
  * ERR_DTYPE; ERR_NULL; ERR_ALIGN.
@@ -395,7 +396,7 @@ mote_status_t mote_block_norm(const mote_block_norm_t* N, const void* y_bf16, in
  *   bias      [N] float or NULL;  act: MOTE_ACT_* (GELU with erf, GELU_TANH its tanh form)
  *   x_bf16    in  [T, K] bf16, row stride ldx elements (ldx >= K, ldx % 8 == 0)
  *   residual  in  [T, N] bf16, row stride ldr elements (ldr >= N), or NULL; may be out itself (bf16, ldr = N)
- *   out       out [T, N] contiguous of out_dtype; must not overlap x
+ *   out       out [T, N] contiguous of out_dtype; must not overlap x, the weights or ws
  *   ws        scratch, >= mote_linear_workspace_bytes(L, T), 256-B aligned; its first word is the device status of
  *             mote_device_status.  Contents need not be kept between calls; two calls that can run at the same time need two.
  * Pointers 16-B aligned.  N is arbitrary; K % 8 == 0 (codes: K % 16 == 0).

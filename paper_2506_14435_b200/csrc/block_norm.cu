@@ -409,9 +409,11 @@ extern "C" mote_status_t mote_block_norm(const mote_block_norm_t* N, const void*
       bad(normed_out, 2, residual, rb, sr) || overlaps(res_out, size_t(T) * d * rb, normed_out, size_t(T) * d * 2))
     return MOTE_ERR_SHAPE;
   const int64_t gate_rows = !N->gate_cols ? 0 : N->gate_tokens ? (T + N->gate_tokens - 1) / N->gate_tokens : 1;
-  const size_t gate_bytes = size_t(gate_rows) * N->gate_cols * (N->gate_dtype == MOTE_DTYPE_F32 ? 4 : 2);
-  if (N->gate_cols && (overlaps(res_out, size_t(T) * d * rb, gate, gate_bytes) || overlaps(normed_out, size_t(T) * d * 2, gate, gate_bytes)))
-    return MOTE_ERR_SHAPE;
+  const void* const read[] = {N->gate_cols ? gate : nullptr, N->post_norm ? N->post_gain : nullptr, N->pre_gain};
+  const size_t read_bytes[] = {size_t(gate_rows) * N->gate_cols * (N->gate_dtype == MOTE_DTYPE_F32 ? 4 : 2), size_t(d) * 4, size_t(d) * 4};
+  for (int i = 0; i < 3; ++i)
+    if (overlaps(res_out, size_t(T) * d * rb, read[i], read_bytes[i]) || overlaps(normed_out, size_t(T) * d * 2, read[i], read_bytes[i]))
+      return MOTE_ERR_SHAPE;
   BlockNormArgs a{};
   a.y = static_cast<const uint16_t*>(y); a.ldy = ldy; a.res = residual; a.ldr = ldr;
   a.gate = N->gate_cols ? gate : nullptr; a.gate_cols = N->gate_cols; a.gate_tokens = N->gate_tokens;

@@ -285,8 +285,12 @@ extern "C" mote_status_t mote_linear(const mote_linear_t* L, const void* x, int6
   if (ws_bytes < mote_linear_workspace_bytes(L, T)) return MOTE_ERR_WORKSPACE;
   const int64_t sx = T > 1 ? ldx : L->K, sr = T > 1 ? ldr : L->N;
   const size_t out_bytes = size_t(T) * L->N * (out_dtype == MOTE_DTYPE_F32 ? 4 : 2);
-  // the output may take the residual's place element by element; x is read by every tile
-  if (ranges_overlap(out, out_bytes, x, size_t((T - 1) * sx + L->K) * 2)) return MOTE_ERR_SHAPE;
+  // the output may take the residual's place element by element; x, the weights and the workspace are read by every tile
+  const void* const read[] = {x, L->W, bits == MOTE_SHARED_BF16 ? nullptr : L->w_scale, L->bias, ws};
+  const size_t read_bytes[] = {size_t((T - 1) * sx + L->K) * 2, size_t(L->N) * L->K * bits / 8, size_t(L->N) * 4, size_t(L->N) * 4,
+                               mote_linear_workspace_bytes(L, T)};
+  for (int i = 0; i < 5; ++i)
+    if (ranges_overlap(out, out_bytes, read[i], read_bytes[i])) return MOTE_ERR_SHAPE;
   if (ranges_overlap(out, out_bytes, residual, size_t((T - 1) * sr + L->N) * 2) &&
       !(out == residual && out_dtype == MOTE_DTYPE_BF16 && sr == L->N))
     return MOTE_ERR_SHAPE;

@@ -330,3 +330,24 @@ def test_operators_on_tensors_that_require_grad(mote):
             call()
     with torch.no_grad():
         assert torch.equal(mote.mote_linear(lin, x, residual=res), mote.mote_linear(lin, plain, residual=res.detach()))
+
+
+def test_operators_on_outputs_next_to_what_they_read(mote):
+    """Side by side in one buffer is no overlap."""
+    d, T = 128, 6
+    buf = torch.zeros(4 * d + 2 * T * d, device="cuda")
+    buf[:2 * d] = 1.0 + 0.1 * _randn(281, 2 * d)
+    y, res = _randn(282, T, d).bfloat16(), _randn(283, T, d)
+    want = mote.mote_block_norm(mote.MoteBlockNorm(d, post_norm=True, post_gain=buf[:d].clone(), pre_gain=buf[d:2 * d].clone()), y, res)
+    norm = mote.MoteBlockNorm(d, post_norm=True, post_gain=buf[:d], pre_gain=buf[d:2 * d])
+    r = mote.mote_block_norm(norm, y, res, res_out=buf[2 * d:2 * d + T * d].view(T, d))
+    assert torch.equal(r[0], want[0]) and torch.equal(r[1], want[1])
+    with pytest.raises(mote.MoteError):
+        mote.mote_block_norm(norm, y, res, res_out=buf[2 * d - 4:2 * d - 4 + T * d].view(T, d))
+    W = _randn(284, d, d).bfloat16()
+    want = mote.mote_linear(mote.MoteLinear(W, bias=buf[:d].clone()), y, out_dtype=torch.float32)
+    lin = mote.MoteLinear(W, bias=buf[:d])
+    got = mote.mote_linear(lin, y, out=buf[d:d + T * d].view(T, d))
+    assert torch.equal(got, want)
+    with pytest.raises(mote.MoteError):
+        mote.mote_linear(lin, y, out=buf[d - 4:d - 4 + T * d].view(T, d))

@@ -1,4 +1,5 @@
 """The binding of the operators around the experts, on the host: what it needs, what it refuses, how its extension module is built."""
+import ctypes as C
 import os
 import subprocess
 import sys
@@ -103,3 +104,29 @@ def test_tensors_that_require_grad_are_refused_where_grad_is_recorded(b):
         with torch.no_grad(), pytest.raises(Exception) as e:       # not on a GPU
             call(x)
         assert "requires grad" not in str(e.value)
+
+
+def test_outputs_over_weights_and_workspaces_are_refused(b):
+    """On the host, before anything is launched; the addresses are never dereferenced."""
+    SHAPE, row = 2, 256 * 4
+
+    def norm(res_out=0x300000, normed=0x400000, **kw):
+        f = dict(d=256, eps=1e-6, scale=1.0, post_norm=1, post_gain=0x500000, pre_gain=0x600000, res_dtype=1, gate_cols=0, gate_dtype=0,
+                 gate_sigmoid=0, gate_tokens=1)
+        f.update(kw)
+        n = C.byref(b.mote_block_norm_t(*[f[k] for k, _ in b.mote_block_norm_t._fields_]))
+        return b.lib.mote_block_norm(n, 0x100000, 256, 0x200000, 256, None, 4, res_out, normed, None)
+
+    for gain in (0x500000, 0x600000):                       # a gain of 1 KB, outputs of 2 KB
+        for at in (gain, gain + row - 16, gain - 2 * row + 16):
+            assert norm(res_out=at) == SHAPE and norm(normed=at) == SHAPE, hex(at)
+
+    def linear(out, bits=8, **kw):
+        f = dict(N=128, K=256, W=0x500000, bits=bits, w_scale=0x600000, bias=0x700000, act=0)
+        f.update(kw)
+        l = C.byref(b.mote_linear_t(*[f[k] for k, _ in b.mote_linear_t._fields_]))
+        return b.lib.mote_linear(l, 0x200000, 256, 100, None, 0, out, 1, 0x800000, 1 << 20, None)
+
+    for at in (0x500000, 0x500000 + 128 * 256 - 16, 0x600000, 0x700000 + 512 - 16, 0x800000, 0x800000 + 256 + 128 * 512 - 16, 0x800000 - 16):
+        assert linear(at) == SHAPE, hex(at)
+    assert linear(0x500000 + 128 * 256, bits=16) == SHAPE   # bf16 weights take twice as much
