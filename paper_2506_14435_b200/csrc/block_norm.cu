@@ -408,7 +408,7 @@ extern "C" mote_status_t mote_block_norm(const mote_block_norm_t* N, const void*
   if (bad(res_out, rb, y, 2, sy) || bad(res_out, rb, residual, rb, sr) || bad(normed_out, 2, y, 2, sy) ||
       bad(normed_out, 2, residual, rb, sr) || overlaps(res_out, size_t(T) * d * rb, normed_out, size_t(T) * d * 2))
     return MOTE_ERR_SHAPE;
-  const int64_t gate_rows = !N->gate_cols ? 0 : N->gate_tokens ? (T + N->gate_tokens - 1) / N->gate_tokens : 1;
+  const int64_t gate_rows = !N->gate_cols ? 0 : N->gate_tokens ? (T - 1) / N->gate_tokens + 1 : 1;
   const void* const read[] = {N->gate_cols ? gate : nullptr, N->post_norm ? N->post_gain : nullptr, N->pre_gain};
   const size_t read_bytes[] = {size_t(gate_rows) * N->gate_cols * (N->gate_dtype == MOTE_DTYPE_F32 ? 4 : 2), size_t(d) * 4, size_t(d) * 4};
   for (int i = 0; i < 3; ++i)

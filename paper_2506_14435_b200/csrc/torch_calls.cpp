@@ -130,7 +130,7 @@ PyObject* block_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
     N.gate_dtype = MOTE_DTYPE_F32;
     if (a[4] != Py_None) {
       const at::Tensor& g = tensor(a[4], "gate");
-      const int64_t rows = N.gate_tokens == 0 ? (T > 0 ? 1 : 0) : (T + N.gate_tokens - 1) / N.gate_tokens;
+      const int64_t rows = T == 0 ? 0 : N.gate_tokens == 0 ? 1 : (T - 1) / N.gate_tokens + 1;
       if (g.dim() != 2 || (g.size(1) != 1 && g.size(1) != d) || g.size(0) != rows || !g.is_contiguous() || !g.is_cuda() || g.get_device() != dev)
         throw Refused{"gate: expected contiguous [" + std::to_string(rows) + ", 1] or [" + std::to_string(rows) + ", " + std::to_string(d) + "] on cuda:" +
                       std::to_string(dev)};

@@ -351,3 +351,17 @@ def test_operators_on_outputs_next_to_what_they_read(mote):
     assert torch.equal(got, want)
     with pytest.raises(mote.MoteError):
         mote.mote_linear(lin, y, out=buf[d - 4:d - 4 + T * d].view(T, d))
+
+
+@pytest.mark.parametrize("gate_tokens", [2 ** 63 - 1, 2 ** 40, 7])
+@pytest.mark.parametrize("T", [1, 7, 1300])
+def test_block_norm_a_gate_for_more_tokens_than_there_are(mote, T, gate_tokens):
+    d = 256
+    y, res = _randn(291, T, d).bfloat16(), _randn(292, T, d).bfloat16()
+    rows = (T - 1) // gate_tokens + 1
+    for cols in (1, d):
+        gate = _randn(293, rows, cols)
+        got = mote.mote_block_norm(mote.MoteBlockNorm(d, gate_tokens=gate_tokens), y, res, gate=gate)
+        each = gate[torch.arange(T, device="cuda") // gate_tokens]
+        want = mote.mote_block_norm(mote.MoteBlockNorm(d), y, res, gate=each)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
