@@ -277,6 +277,9 @@ def _vector(t, name: str, n: int, dev):
     return t, t.data_ptr()
 
 
+SCORINGS = {"softmax": 0, "sigmoid": 1}
+
+
 class MoteRouter:
     """A scored router's weights and options (mote_router_t): Wr[E, d] fp32 or bf16; scoring "softmax" or "sigmoid"; logit_bias and
     select_bias[E] fp32.  Construction runs mote_router_pack; make a new one when Wr has changed."""
@@ -285,6 +288,8 @@ class MoteRouter:
         _need_cuda(Wr)
         if Wr.dim() != 2 or Wr.dtype not in _DTYPES:
             raise ValueError("Wr: expected a float32 or bfloat16 matrix")
+        if scoring not in SCORINGS:
+            raise ValueError(f"scoring: expected one of {sorted(SCORINGS)}")
         self.E, self.d = Wr.shape
         self.k = k
         self.device = Wr.get_device()
@@ -298,7 +303,7 @@ class MoteRouter:
         packed = torch.empty(need, dtype=torch.uint8, device=Wr.device)
         _check(lib.mote_router_pack(_ptr(Wr), dt, self.E, self.d, _ptr(packed), need, _stream()), "mote_router_pack")
         self.tensors = dict(Wr=Wr, logit_bias=lb, select_bias=sb, packed=packed)
-        self.struct = mote_router_t(self.d, self.E, k, {"softmax": 0, "sigmoid": 1}[scoring], n_groups, topk_groups, int(renorm), scale,
+        self.struct = mote_router_t(self.d, self.E, k, SCORINGS[scoring], n_groups, topk_groups, int(renorm), scale,
                                     Wr.data_ptr(), dt, lb_ptr, sb_ptr, packed.data_ptr())
         self._address = C.addressof(self.struct)
 

@@ -90,6 +90,7 @@ PyObject* route_scored(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const auto* R = static_cast<const mote_router_t*>(PyLong_AsVoidPtr(a[0]));
     const int64_t dev = PyLong_AsLongLong(a[1]);
     const at::Tensor& x = tensor(a[2], "x");
+    if (const int st = mote_route_scored(R, nullptr, 0, 0, nullptr, nullptr, nullptr, nullptr)) return PyLong_FromLong(st);   // k, ahead of [T, k]
     on_current_device(dev);
     const int64_t T = rows_of(x, "x"), ldx = row_stride(x, "x", at::kBFloat16, T, R->d, dev);
     at::Tensor idx = fresh(T, R->k, at::kInt, dev), w = fresh(T, R->k, at::kFloat, dev), logits;

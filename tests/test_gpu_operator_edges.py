@@ -365,3 +365,12 @@ def test_block_norm_a_gate_for_more_tokens_than_there_are(mote, T, gate_tokens):
         each = gate[torch.arange(T, device="cuda") // gate_tokens]
         want = mote.mote_block_norm(mote.MoteBlockNorm(d), y, res, gate=each)
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_routers_that_are_refused(mote):
+    Wr, x = _randn(301, 16, 64), _randn(302, 3, 64).bfloat16()
+    with pytest.raises(ValueError, match="scoring"):
+        mote.MoteRouter(Wr, 2, scoring="tanh")
+    for bad in (dict(k=0), dict(k=-3), dict(k=2 ** 31 - 1), dict(k=2, n_groups=3), dict(k=2, n_groups=4, topk_groups=5), dict(k=2, scale=float("nan"))):
+        with pytest.raises(mote.MoteError):
+            mote.mote_route_scored(mote.MoteRouter(Wr, **bad), x)

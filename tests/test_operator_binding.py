@@ -130,3 +130,17 @@ def test_outputs_over_weights_and_workspaces_are_refused(b):
     for at in (0x500000, 0x500000 + 128 * 256 - 16, 0x600000, 0x700000 + 512 - 16, 0x800000, 0x800000 + 256 + 128 * 512 - 16, 0x800000 - 16):
         assert linear(at) == SHAPE, hex(at)
     assert linear(0x500000 + 128 * 256, bits=16) == SHAPE   # bf16 weights take twice as much
+
+
+@pytest.mark.parametrize("bad", [dict(k=0), dict(k=-3), dict(k=2 ** 31 - 1), dict(n_groups=3), dict(topk_groups=0), dict(scoring=7)])
+def test_a_router_that_the_library_refuses_is_refused_before_outputs_are_made(b, bad):
+    f = dict(d=64, E=16, k=2, scoring=1, n_groups=1, topk_groups=1, renorm=1, scale=1.0, Wr=0x100000, w_dtype=0, logit_bias=None, select_bias=None,
+             packed=0x100000)
+    f.update(bad)
+
+    class Router:
+        device, struct = 0, b.mote_router_t(*[f[n] for n, _ in b.mote_router_t._fields_])
+        _address = C.addressof(struct)
+
+    with pytest.raises(b.MoteError):
+        b.mote_route_scored(Router, torch.zeros(3, 64, dtype=torch.bfloat16))
