@@ -461,8 +461,9 @@ mote_status_t mote_moe_forward_profile(const mote_layer_t* L, const void* x_bf16
  * kernels has a time limit; a CTA whose wait runs out stops working, lets copies in flight land,
  * releases its tensor memory, raises this word and returns normally, so the context stays usable
  * and the output of that call is invalid).  Synchronises the stream itself.
- * The word is cleared at the start of every mote_moe_forward / mote_moe_forward_host call and once
- * at the start of mote_stack_forward (not between its layers), so it reports the last such call. */
+ * The word is cleared at the start of every mote_moe_forward / mote_moe_forward_scored / mote_moe_forward_host / mote_linear
+ * call and once at the start of mote_stack_forward (not between its layers), so it reports the last such call.
+ * mote_route_scored's, in `packed`, is cleared by mote_router_pack and here only: it reports all calls since. */
 mote_status_t mote_device_status(void* ws, void* stream);
 
 /* Diagnostic for the mechanism above (no counterpart in the paper): enqueues one thread block that

@@ -307,6 +307,11 @@ class MoteRouter:
                                     Wr.data_ptr(), dt, lb_ptr, sb_ptr, packed.data_ptr())
         self._address = C.addressof(self.struct)
 
+    def check_device_status(self):
+        """Raises MoteError if a bounded device-side wait has run out in a call since this was last asked (the outputs of that call are
+        invalid).  Waits for the current stream."""
+        _check(lib.mote_device_status(_ptr(self.tensors["packed"]), _stream()), "MoteRouter (device)")
+
 
 def mote_route_scored(router: MoteRouter, x: torch.Tensor, want_logits: bool = False):
     """x[T, d] bf16 (rows may be strided) -> (topk_idx int32[T, k], topk_w f32[T, k], logits f32[T, E] or None)."""
@@ -384,6 +389,12 @@ class MoteLinear:
                 self._ws_address, self._ws_bytes = self._ws.data_ptr(), need
             self._ws_T = T
         return self._ws
+
+    def check_device_status(self):
+        """Raises MoteError if a bounded device-side wait has run out in the last call (each clears the word; the outputs of that call are
+        invalid).  Waits for the current stream."""
+        if self._ws is not None:
+            _check(lib.mote_device_status(_ptr(self._ws), _stream()), "MoteLinear (device)")
 
 
 def mote_linear(linear: MoteLinear, x: torch.Tensor, residual=None, out=None, out_dtype=torch.bfloat16):

@@ -374,3 +374,27 @@ def test_routers_that_are_refused(mote):
     for bad in (dict(k=0), dict(k=-3), dict(k=2 ** 31 - 1), dict(k=2, n_groups=3), dict(k=2, n_groups=4, topk_groups=5), dict(k=2, scale=float("nan"))):
         with pytest.raises(mote.MoteError):
             mote.mote_route_scored(mote.MoteRouter(Wr, **bad), x)
+
+
+@pytest.mark.parametrize("T", [3, 400])
+def test_device_status_through_the_objects(mote, T):
+    """The word that a wait that ran out raises is set by the library's own wait on nothing, with a limit of 1 ms."""
+    x = _randn(311, T, 64).bfloat16()
+    lin, router = mote.MoteLinear(_randn(312, 64, 64).bfloat16()), mote.MoteRouter(_randn(313, 8, 64), 2)
+    lin.check_device_status()                                   # no workspace yet
+    mote.mote_linear(lin, x)
+    mote.mote_route_scored(router, x)
+    lin.check_device_status()
+    router.check_device_status()
+    for obj, word in ((lin, lin._ws), (router, router.tensors["packed"])):
+        assert mote.lib.mote_selftest_bounded_wait(word.data_ptr(), 1000000, None) == 0
+        with pytest.raises(mote.MoteError) as e:
+            obj.check_device_status()
+        assert e.value.status == 7
+        obj.check_device_status()
+        assert mote.lib.mote_selftest_bounded_wait(word.data_ptr(), 1000000, None) == 0
+    mote.mote_linear(lin, x)                                    # clears its own
+    lin.check_device_status()
+    mote.mote_route_scored(router, x)                           # stays until it is read
+    with pytest.raises(mote.MoteError):
+        router.check_device_status()
