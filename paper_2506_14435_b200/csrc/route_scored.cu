@@ -224,13 +224,13 @@ __device__ __forceinline__ void choose_experts(const ScoredRouter& r, const Lane
     for (int j = 0; j < r.topk_groups; ++j) kept |= 1ull << groups.take(last, lane);
     if (r.topk_groups < G) {
       groups.take(best, lane);
-      const float worst = key_value(last);
+      const float worst = key_value(last), bound = delta > 1e30f ? 1e30f : delta;     // (infinite for a norm beyond fp32; 0 times it is 0)
       float reach = 4.0f * tau + 2.4e-7f * finite_abs(worst), two_taus = 2.0f * tau;
       if (ratios) {
         // e^x is off by its logit's error and by a few 2^-24 |x| (x: the logit less the largest one), relative to its size; a sum's |x| is
         // that of its larger part, no more than |log(sum / largest score)| + 1 and, weighted, as much again for the smaller part.  The
         // last part: scores too small for fp32.
-        const float rel = delta + 1e-6f + 2e-7f * fminf(1.0f - __logf(fmaxf(worst / smax, 1e-38f)), 110.0f);
+        const float rel = bound + 1e-6f + 2e-7f * fminf(1.0f - __logf(fmaxf(worst / smax, 1e-38f)), 110.0f);
         reach = rel * (worst + key_value(best)) + 1e-36f;
         two_taus = 0.0f;                           // (the floors below are relative too)
       }
@@ -244,7 +244,7 @@ __device__ __forceinline__ void choose_experts(const ScoredRouter& r, const Lane
         if (__popcll(d.border) > kMaxBorder) {
           d.full = 1;
         } else {
-          const float shrink = ratios ? 1.0f - 2.0f * (delta + 3e-5f) : 1.0f;
+          const float shrink = ratios ? 1.0f - 2.0f * (bound + 3e-5f) : 1.0f;
           second0 = second0 * shrink - two_taus;   // floors
           second1 = second1 * shrink - two_taus;
           auto part_of = [&](bool there, int g, float c) {
@@ -297,7 +297,8 @@ __device__ __forceinline__ void choose_experts(const ScoredRouter& r, const Lane
     };
     d.chosen = all_of(chosen);
     d.which = which = all_of(which);
-    d.settled = d.full ? (E == 64 ? ~0ull : (1ull << E) - 1ull) : d.settled | which;
+    d.settled |= which;
+    if (d.full || !d.settled) { d.full = 1; d.settled = E == 64 ? ~0ull : (1ull << E) - 1ull; }      // (none: NaN)
     return;
   }
   const float a = __shfl_sync(0xffffffffu, p0, expert & 31), b = __shfl_sync(0xffffffffu, p1, expert & 31);

@@ -165,6 +165,47 @@ def test_route_scored_logits_within_the_bound_the_choice_relies_on(mote, tokens,
         assert np.all(np.abs(_f64(w) - ref["w"]) <= rel * ref["w"])
 
 
+@pytest.mark.parametrize("tokens", [4, 70, 1200])
+@pytest.mark.parametrize("scoring,n_groups,topk_groups,bias", [("softmax", 1, 1, False), ("softmax", 8, 3, False), ("softmax", 16, 5, False),
+                                                               ("softmax", 8, 3, True), ("sigmoid", 1, 1, True), ("sigmoid", 8, 3, False),
+                                                               ("sigmoid", 16, 5, True)])
+@pytest.mark.parametrize("size", [1e22, 1e-24, 1.0])
+def test_route_scored_tokens_whose_squares_leave_fp32(mote, tokens, scoring, n_groups, topk_groups, bias, size):
+    """Their norm is infinite or its square vanishes, their logits are ordinary (some far apart, so that scores vanish): nothing is known of the
+    errors, everything is evaluated."""
+    E, d = 64, 1024
+    x = _randn(321, tokens, d) * size
+    x[::2] *= 60.0
+    sb = _randn(323, E) * 0.02 if bias else None
+    Wr = _randn(322, E // 2, d).repeat(2, 1) * (0.05 / size)
+    Wr[E // 2:] += (torch.rand(E // 2, d, generator=torch.Generator("cuda").manual_seed(324), device="cuda") - 0.5) * (2.0 ** -24 / size)
+    opt = dict(scoring=scoring, n_groups=n_groups, topk_groups=topk_groups)
+    idx, w, _ = mote.mote_route_scored(mote.MoteRouter(Wr, 4, select_bias=sb, **opt), x.bfloat16())
+    ref = O.route_scored(_f64(x.bfloat16()), _f64(Wr), 4, select_bias=_f64(sb), **opt)
+    assert np.array_equal(idx.cpu().numpy(), ref["idx"])
+    assert np.all(np.isfinite(_f64(w)))
+
+
+@pytest.mark.parametrize("tokens", [1, 33, 1200])
+@pytest.mark.parametrize("alike", [2, 3, 5, 8, 16])
+@pytest.mark.parametrize("scoring,bias", [("softmax", False), ("softmax", True), ("sigmoid", False), ("sigmoid", True)])
+def test_route_scored_several_groups_alike(mote, tokens, alike, scoring, bias):
+    """Groups whose sums differ in their last bits: any number of them at the border between those that stay and the rest."""
+    E, d, G = 64, 512, 16
+    x = _randn(331, tokens, d).bfloat16()
+    Wr = _randn(332, G, E // G, d) * 0.05
+    Wr[:alike] = Wr[:1]
+    Wr[:alike] += (torch.rand(alike, E // G, d, generator=torch.Generator("cuda").manual_seed(333), device="cuda") - 0.5) * 2.0 ** -25
+    Wr = Wr.view(E, d)[torch.randperm(G, generator=torch.Generator().manual_seed(334)).repeat_interleave(4).cuda() * 4 +
+                       torch.arange(4, device="cuda").repeat(G)].contiguous()
+    sb = (_randn(335, 4) * 0.05).repeat(G) if bias else None
+    for topk_groups in (1, 4, 9):
+        opt = dict(scoring=scoring, n_groups=G, topk_groups=topk_groups)
+        idx = mote.mote_route_scored(mote.MoteRouter(Wr, 4, select_bias=sb, **opt), x)[0]
+        ref = O.route_scored(_f64(x), _f64(Wr), 4, select_bias=_f64(sb), **opt)
+        assert np.array_equal(idx.cpu().numpy(), ref["idx"])
+
+
 # ------------------------------------------------------------------------------------------------ projections
 ACTS = ["none", "relu", "silu", "gelu", "gelu_tanh"]
 
