@@ -50,6 +50,12 @@ void* out_pointer(const at::Tensor& t, const char* name, at::ScalarType type, in
   return t.data_ptr();
 }
 
+bool truth(PyObject* o) {
+  const int v = PyObject_IsTrue(o);
+  if (v < 0) throw python_error();
+  return v != 0;
+}
+
 int dtype_code(at::ScalarType t, const char* name) {
   if (t == at::kFloat) return MOTE_DTYPE_F32;
   if (t == at::kBFloat16) return MOTE_DTYPE_BF16;
@@ -94,7 +100,7 @@ PyObject* route_scored(PyObject*, PyObject* const* args, Py_ssize_t n) {
     on_current_device(dev);
     const int64_t T = rows_of(x, "x"), ldx = row_stride(x, "x", at::kBFloat16, T, R->d, dev);
     at::Tensor idx = fresh(T, R->k, at::kInt, dev), w = fresh(T, R->k, at::kFloat, dev), logits;
-    if (PyObject_IsTrue(a[3])) logits = fresh(T, R->E, at::kFloat, dev);
+    if (truth(a[3])) logits = fresh(T, R->E, at::kFloat, dev);
     const int st = mote_route_scored(R, x.data_ptr(), ldx, T, static_cast<int32_t*>(idx.data_ptr()), static_cast<float*>(w.data_ptr()),
                                      logits.defined() ? static_cast<float*>(logits.data_ptr()) : nullptr, stream_of(dev));
     if (st) return PyLong_FromLong(st);
@@ -143,8 +149,8 @@ PyObject* block_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
     void *r_out = nullptr, *n_out = nullptr;
     if (a[5] != Py_None) r_out = out_pointer(tensor(a[5], "res_out"), "res_out", stream_type, T, d, dev);
     if (a[6] != Py_None) n_out = out_pointer(tensor(a[6], "normed_out"), "normed_out", at::kBFloat16, T, d, dev);
-    if (!r_out && a[5] == Py_None && PyObject_IsTrue(a[7])) { made_r = fresh(T, d, stream_type, dev); r_out = made_r.data_ptr(); }
-    if (!n_out && a[6] == Py_None && PyObject_IsTrue(a[8])) { made_n = fresh(T, d, at::kBFloat16, dev); n_out = made_n.data_ptr(); }
+    if (!r_out && a[5] == Py_None && truth(a[7])) { made_r = fresh(T, d, stream_type, dev); r_out = made_r.data_ptr(); }
+    if (!n_out && a[6] == Py_None && truth(a[8])) { made_n = fresh(T, d, at::kBFloat16, dev); n_out = made_n.data_ptr(); }
     const int st = mote_block_norm(&N, y.data_ptr(), ldy, res, ldr, gate, T, r_out, n_out, stream_of(dev));
     if (st) return PyLong_FromLong(st);
     auto result = [](PyObject* given, const at::Tensor& made) {

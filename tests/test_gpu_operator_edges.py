@@ -439,3 +439,15 @@ def test_device_status_through_the_objects(mote, T):
     mote.mote_route_scored(router, x)                           # stays until it is read
     with pytest.raises(mote.MoteError):
         router.check_device_status()
+
+
+def test_flags_that_have_no_truth_value(mote):
+    """Their own error comes through."""
+    two = torch.tensor([1, 0])
+    x = _randn(341, 3, 64).bfloat16()
+    with pytest.raises(RuntimeError, match="ambiguous"):
+        mote.mote_route_scored(mote.MoteRouter(_randn(342, 8, 64), 2), x, want_logits=two)
+    for bad in (dict(want_residual=two), dict(want_normed=two)):
+        with pytest.raises(RuntimeError, match="ambiguous"):
+            mote.mote_block_norm(mote.MoteBlockNorm(64), x, **bad)
+    assert mote.mote_route_scored(mote.MoteRouter(_randn(342, 8, 64), 2), x, want_logits=0)[2] is None
