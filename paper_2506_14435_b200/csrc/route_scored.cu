@@ -693,8 +693,8 @@ constexpr int kScoredTokens = 16;
 // NE: 8-expert column tiles (ceil(E / 8) rounded up to 1, 2, 4 or 8); kF32: type of the router weights.
 // Lane (g, t) = (lane / 4, lane % 4) loads elements [32 * step + 8 * t, + 8) of token rows g and g + 8 and of router rows 8n + g;
 // the reduction index may be permuted as long as both operands are.
-// kAlone: a CTA has its SM to itself, and registers for all sums of 64 experts (512 x 2048: 14.4 us, 16.6 with half of them); two share one
-// where CTAs are more (4096 x 256: 15.9 us, 20.5 one after the other).
+// kAlone: a CTA has its SM to itself, and registers for all sums of 64 experts: where the clusters run at a time so (512 x 2048: 11.7 us, 14.2
+// with half of them; 256 x 2048, whose 16 clusters of eight do not: 14.7 us in two rounds, 12.2 with two CTAs an SM).
 template <int NE, bool kF32, bool kAlone>
 __global__ void __launch_bounds__(kScoredWarps * 32, kAlone ? 1 : 2) route_scored_kernel(const __grid_constant__ ScoredRouter r, int cluster) {
   __shared__ union {
@@ -1086,14 +1086,16 @@ static bool router_ok(const mote_router_t* R) {
 }
 
 template <int NE, bool kF32>
-static cudaError_t launch_scored_as(const ScoredRouter& r, unsigned grid, int cluster, cudaStream_t stream) {
-  return (int)grid <= device_sm_count()
-             ? launch_ex(route_scored_kernel<NE, kF32, true>, dim3(grid), dim3(kScoredWarps * 32), 0, stream, true, cluster, r, cluster)
-             : launch_ex(route_scored_kernel<NE, kF32, false>, dim3(grid), dim3(kScoredWarps * 32), 0, stream, true, cluster, r, cluster);
+static cudaError_t launch_scored_as(const ScoredRouter& r, unsigned tiles, int cluster, cudaStream_t stream) {
+  static ResidentClusters resident;
+  const int alone = cluster > 1 ? resident.get(route_scored_kernel<NE, kF32, true>, kScoredWarps * 32, 0, cluster) : device_sm_count();
+  const dim3 grid(tiles * cluster), block(kScoredWarps * 32);
+  return (int64_t)tiles <= alone ? launch_ex(route_scored_kernel<NE, kF32, true>, grid, block, 0, stream, true, cluster, r, cluster)
+                                 : launch_ex(route_scored_kernel<NE, kF32, false>, grid, block, 0, stream, true, cluster, r, cluster);
 }
 template <int NE>
 static cudaError_t launch_scored(const ScoredRouter& r, unsigned tiles, int cluster, cudaStream_t stream) {
-  return r.w_f32 ? launch_scored_as<NE, true>(r, tiles * cluster, cluster, stream) : launch_scored_as<NE, false>(r, tiles * cluster, cluster, stream);
+  return r.w_f32 ? launch_scored_as<NE, true>(r, tiles, cluster, stream) : launch_scored_as<NE, false>(r, tiles, cluster, stream);
 }
 
 static cudaError_t launch_tiles(const ScoredRouter& r, const CUtensorMap& tx, const CUtensorMap& tw, int experts, int terms, uint32_t* status,
@@ -1113,9 +1115,9 @@ static cudaError_t launch_tiles(const ScoredRouter& r, const CUtensorMap& tx, co
 }
 
 // The logits come from the tcgen05 kernel from this much work on: tokens x width x column tiles of 8 experts x bf16 terms of the weights.  us,
-// warp-level MMAs / tcgen05, 64 experts in fp32: 512 x 2048 12.8 / 13.6, 1024 x 2048 19 / 16, 8192 x 2048 67 / 28, 4096 x 256 12.7 / 17,
-// 8192 x 256 21 / 17; 16 experts in fp32: 2048 x 2048 14.7 / 16.5, 8192 x 1024 21 / 19; 32 in bf16: 4096 x 2048 15.6 / 16.8, 8192 x 2048 27 / 23.
-// Over 240 such shapes the rule is within 14 % of the better one, 0.3 % on average (without the width: 2.1 times and 6 %).
+// warp-level MMAs / tcgen05, 64 experts in fp32: 512 x 2048 11.7 / 15.3, 700 x 2048 14.9 / 15.2, 1024 x 2048 15.0 / 15.6, 8192 x 2048 67 / 25,
+// 4096 x 256 12.8 / 15.6, 8192 x 256 21.4 / 15.8; 16 experts in fp32: 2048 x 2048 12.9 / 16.0, 8192 x 1024 20.5 / 17.9; 32 in bf16: 4096 x 2048
+// 15.2 / 15.7, 8192 x 2048 26.2 / 20.9.
 constexpr int64_t kTileMinWork = 30000000;
 
 // status: the device status word that a bounded wait raises; null: the router's own
