@@ -464,7 +464,8 @@ linear_umma_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
 // ------------------------------------------------------------------------------------------------
 // Which form and tile width: the least estimated time, in cycles.  The estimate's constants were fitted to times of all forms at 79
 // sizes (17 to 8192 tokens, 26 to 11008 rows, K 128 to 11008): the form that it names is 0.9 % slower than the best one on average and
-// 16 % at worst (2048 x 2048 x 2048: pairs of 256, 18.1 us, single CTAs of 240 15.7).  Tokens x N x K: 4096 x 11008 x 2048: pairs of 256, 122 us
+// 16 % at worst (2048 x 2048 x 2048: pairs of 256, 18.1 us, single CTAs of 240 15.7).  Times of those runs, one size back to back (as calls among
+// others the first two below take 150 and 14.9 us).  Tokens x N x K: 4096 x 11008 x 2048: pairs of 256, 122 us
 // (single CTAs 133), 333 x 8960 x 1536: single CTAs of 192, 13.6 us (pairs 16), 64 x 2048 x 2048: tiles of 64 split four ways, 8.4 us (whole 10).
 struct LinearForm { int cg, bn, splits; };
 static LinearForm pick_form(int64_t T, int64_t N, int k_steps, int sms, const int (&clusters)[9]) {

@@ -835,10 +835,11 @@ __global__ void __launch_bounds__(kScoredWarps * 32, kAlone ? 1 : 2) route_score
 // Warps: 0 TMA producer, 1 MMA issuer, 2 TMEM owner, 4 to 19 epilogue (four per TMEM lane quarter, 16 experts each), 20 to 27 norms;
 // all 32 choose.
 //
-// 8192 x 2048, 64 experts in 8 groups, fp32 Wr: 29.1 us in a graph (27.7 with sums of 64 elements added without compensation, whose bound did not hold), where the bytes take 5.4.  About 11 us are the products: 655 KB of
-// operands an SM, three fifths of them the weights' terms, are 6 us at the 61 bytes a cycle that an SM gets, the rest is the start of the
-// pipeline.  7 are the choice, bound by instructions (710 a token, 64 tokens to an SM), 4 second evaluations, latency.
-// The kernel above, whose tokens are 16 to a cluster, takes 78.
+// 8192 x 2048, 64 experts in 8 groups, fp32 Wr: 28.9 us in a graph, where the bytes take 5.4 (27.7 with sums of 64 elements and without
+// compensation, whose bound did not hold).  About 11 us are the products: 655 KB of operands an SM, three fifths of them the weights'
+// terms, are 6 us at the 61 bytes a cycle that an SM gets, the rest is the start of the pipeline.  7 are the choice, bound by instructions
+// (710 a token, 64 tokens to an SM), 4 or 5 second evaluations, latency; the rest is not accounted for.  The kernel above, whose tokens
+// are 16 to a cluster, takes 67.
 // ------------------------------------------------------------------------------------------------
 constexpr int kTileTokens = 128;
 constexpr int kTileWarps = 16, kTileNormWarps = 8, kTileThreads = 1024;
