@@ -212,7 +212,7 @@ mote_status_t mote_route_stats(const float* logits, const int32_t* topk_idx, int
  *   packed  output of mote_router_pack for this Wr, 256-B aligned; its first word is the device status of
  *           mote_device_status, which stays until it is read
  *   x_bf16  in   [T, d] bf16, row stride ldx elements (ldx >= d, ldx % 8 == 0), 16-B aligned
- *   topk_idx out [T, k] int32;  topk_w out [T, k] float;  logits out [T, E] float or NULL
+ *   topk_idx out [T, k] int32;  topk_w out [T, k] float;  logits out [T, E] float or NULL; outputs overlap nothing
  * T = 0 is a no-op.  Errors: T > 2^24, d % 8 != 0, d > 32768, E < 1, E > MOTE_MAX_EXPERTS, k < 1, k > E, k > MOTE_MAX_TOPK, n_groups not
  * a divisor of E, topk_groups not in 1 .. n_groups, k > topk_groups * E / n_groups, unknown scoring, a scale that is not a
  * number -> ERR_SHAPE; ERR_DTYPE; ERR_NULL; ERR_ALIGN.
@@ -352,7 +352,7 @@ mote_status_t mote_rms_norm(const void* x_bf16, int64_t T, int64_t d, float eps,
  *   r' = residual + scale * g * p              g = 1, gate, or 1 / (1 + exp(-gate)) with gate_sigmoid
  *   n  = bf16( r' * rsqrt( mean_j r'[t, j]^2 + eps ) * pre_gain[j] )
  *
- * fp32 arithmetic; r' is rounded once, to the type of the residual stream, and n is the norm of the rounded r' (with unit gain
+ * fp32 arithmetic (the sums of squares have to be finite in it); r' is rounded once, to the type of the residual stream, and n is the norm of the rounded r' (with unit gain
  * and no gate: what mote_rms_norm gives for res_out).  Rows are independent and do not depend on T.
  *
  *   gate  gate_cols = 0: none.  Else [rows, gate_cols] contiguous of gate_dtype with gate_cols = 1 (one gate for all
